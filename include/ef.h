@@ -63,7 +63,7 @@ extern "C" {
                              eta <= 0, eta_prev < 0, non-finite, stride < d or not a multiple of 4 */
 #define EF_ERR_ALIGN -4   /* pointer not aligned as required */
 #define EF_ERR_HIP -5     /* the HIP runtime reported an error (allocation, launch, no device) */
-#define EF_ERR_SIZE -6    /* input beyond the fixed capacity of an entry point that allocates nothing */
+#define EF_ERR_SIZE -6    /* input beyond the fixed capacity of an entry point that allocates nothing, or of a workspace */
 
 #define EF_MAX_WORKERS 64
 
@@ -370,6 +370,166 @@ int ef_worker_step_quality(const ef_plan *plan, int n_workers, const float *grad
 #define EF_QUALITY_STATIC_MAX_TILE_VECTORS 131072
 int ef_compressor_quality_static(const ef_plan *plan, int n_vectors, const float *v, int64_t stride,
                                  double *out, void *stream);
+
+/*
+ * A worker's forward and backward pass
+ * ------------------------------------
+ * Operators that make a worker's gradient: RMS norm, checkpoints of
+ * activations in 8 bits, the weight gradient of a linear layer taken from such
+ * a checkpoint, and the clipped policy loss on a language model's logits.  They
+ * read parameters and write parameter gradients where the step calls have
+ * them: fp32, anywhere in the flat d-vector (`weight`, `dweight`, `dw` and the
+ * other fp32 vectors of these calls need 4-byte alignment only).
+ *
+ * Matrices are row-major, one row to a token, `rows` >= 0 of them, of `type`
+ * EF_TYPE_FP32 or EF_TYPE_BF16, aligned to their element, rows `*_stride` elements
+ * apart (>= the row's length; not used and not checked with fewer than two
+ * rows).  All calls enqueue on `stream`, allocate nothing, record no memset and
+ * may be captured into a HIP graph.  Outputs may share memory neither with each
+ * other nor with inputs (EF_ERR_ARG), except where a call says "in place": there the same
+ * pointer with the same stride may be given.  Two matrices whose rows lie side
+ * by side in one buffer (same stride, different columns) do not share memory.
+ * Sums, means and products are accumulated in fp32 or wider in a fixed order:
+ * repeated calls give the same bits.  Infinities and NaN go where the formulas
+ * take them.  rows = 0 is a valid call: sums over no rows are zero.
+ */
+#define EF_TYPE_FP32 0
+#define EF_TYPE_BF16 1
+
+/*
+ * Checkpoint of a matrix [rows][width] in 8 bits: one buffer (device, 16-byte aligned)
+ * of ef_act_bytes(rows, width) bytes,
+ *     codes   uint8[rows][G * 32], G = ceil(width / 32): E4M3 numbers, 0 behind the row's end
+ *     scales  uint8[rows][G], from byte ef_act_scales_offset(rows, width) = rows * G * 32 on:
+ *             E8M0, value 2^(byte - 127), one for every 32 consecutive elements of a row
+ *     padding up to a multiple of 16 bytes, never read, never written
+ * An element stands for code * scale.  The scale is the least power of two 2^e, e in
+ * [-117, 119], that brings the group's largest magnitude to 448 (E4M3's largest) or below;
+ * codes are rounded to nearest even (and held to 448 in size if e ended at 119).  What a
+ * checkpoint stands for is therefore a bf16 number exactly.  A group that holds
+ * an infinity or NaN gets scale byte 255 and codes that read as NaN.
+ * Both functions return 0 for rows < 0, width < 1, or sizes beyond 2^62 bytes.
+ */
+size_t ef_act_bytes(int64_t rows, int64_t width);
+size_t ef_act_scales_offset(int64_t rows, int64_t width);
+
+/* act <- checkpoint of x;  y <- what act stands for (exact in either type). */
+int ef_act_encode(int64_t rows, int64_t width, int type, const void *x, int64_t x_stride, void *act, void *stream);
+int ef_act_decode(int64_t rows, int64_t width, const void *act, int type, void *y, int64_t y_stride, void *stream);
+
+/*
+ * RMS norm with the residual's addition and an 8-bit output.  For every row
+ *     v    = x + residual                          (fp32; v = x without a residual)
+ *     rstd = 1 / sqrt(mean(v^2) + eps)
+ *     xhat = v * rstd
+ *     h   <- v,  y <- xhat * weight                (each rounded once to `type`)
+ *     act <- checkpoint of xhat
+ * The checkpoint is of the normalised row before the weight: one buffer then
+ * serves the norm's backward pass and, with the weight as the columns' factor, the weight
+ * gradient of the linear layer that reads y (ef_weight_grad), and neither h nor
+ * y has to be kept.
+ *
+ *   x         in   type[rows][x_stride]
+ *   residual  in   the same, or NULL
+ *   weight    in   float[width], or NULL for ones
+ *   h, y      out  type[rows][..], either may be NULL; in place over x or residual
+ *   act       out  ef_act_bytes(rows, width) bytes, or NULL
+ *   rstd      out  float[rows], or NULL
+ * eps >= 0 and finite, 1 <= width <= EF_NORM_MAX_WIDTH (EF_ERR_SIZE beyond); one output at
+ * least (EF_ERR_NULL).
+ */
+#define EF_NORM_MAX_WIDTH 16384
+int ef_norm_forward(int64_t rows, int64_t width, int type, const void *x, int64_t x_stride, const void *residual,
+                    int64_t residual_stride, const float *weight, float eps, void *h, int64_t h_stride, void *y,
+                    int64_t y_stride, void *act, float *rstd, void *stream);
+
+/*
+ * Workspace of the calls below: row sums and partial results, no state between
+ * calls.  Calls that share one must be ordered on the device and run on the
+ * device it was created on (EF_ERR_ARG otherwise).  Takes 64 MiB and
+ * 16 bytes a row.  Creation allocates (hipMalloc) and synchronises;
+ * ef_workspace_destroy synchronises the device.
+ *
+ *   max_rows  most rows of a later call (EF_ERR_SIZE for more), 0 .. 2^31 - 1
+ */
+typedef struct ef_workspace ef_workspace; /* opaque */
+int ef_workspace_create(ef_workspace **out, int64_t max_rows, void *stream);
+int ef_workspace_destroy(ef_workspace *workspace);
+
+/*
+ * Backward pass of ef_norm_forward from its checkpoint.  xhat is what act
+ * stands for, dy the gradient of y, dh that of h on the residual's path:
+ *     g        = dy * weight
+ *     dx      <- dh + rstd * (g - xhat * mean(g * xhat))    (of x and of residual alike)
+ *     dweight <- [dweight +] sum over rows of dy * xhat
+ *
+ *   dy       in   type[rows][dy_stride]
+ *   act      in   checkpoint of [rows][width]
+ *   rstd     in   float[rows]
+ *   weight   in   float[width], or NULL for ones
+ *   dh       in   type[rows][dh_stride], or NULL for zeros
+ *   dx       out  type[rows][dx_stride]; in place over dy or dh
+ *   dweight  out  float[width], or NULL; accumulate != 0: added to what it holds
+ */
+int ef_norm_backward(ef_workspace *workspace, int64_t rows, int64_t width, int type, const void *dy, int64_t dy_stride,
+                     const void *act, const float *rstd, const float *weight, const void *dh, int64_t dh_stride,
+                     void *dx, int64_t dx_stride, float *dweight, int accumulate, void *stream);
+
+/*
+ * Weight gradient of a linear layer z = x * W^T from a checkpoint of its input:
+ *     dw[o][i] <- [dw[o][i] +] column_scale[i] * sum over rows t of dz[t][o] * act[t][i]
+ * on matrix instructions, accumulated in fp32.  What a checkpoint stands for and
+ * bf16 gradients enter exactly; fp32 gradients enter as the sum of three bf16 numbers,
+ * which holds all their 24 bits (parts below bf16's least normal number, 2^-126, are lost).
+ *
+ *   dz            in   type[rows][dz_stride], rows of out_width
+ *   act           in   checkpoint of [rows][width]
+ *   column_scale  in   float[width] (the norm's weight where act is ef_norm_forward's), or NULL for ones
+ *   dw            out  float[out_width][width], contiguous; accumulate != 0: added to what it holds
+ * out_width and width from 1 to 2^24.
+ */
+int ef_weight_grad(ef_workspace *workspace, int64_t rows, int64_t out_width, int64_t width, int type, const void *dz,
+                   int64_t dz_stride, const void *act, const float *column_scale, float *dw, int accumulate, void *stream);
+
+/*
+ * Log-probability of each row's token under softmax(logits):
+ *     logp[t] <- logits[t][tokens[t]] - log(sum_v exp(logits[t][v]))
+ * 0 for a token outside [0, vocab), whose row is not read.
+ *
+ *   logits  in   type[rows][stride], rows of vocab entries, 1 <= vocab < 2^31; -inf rules an entry out
+ *   tokens  in   int64[rows], 8-byte aligned
+ *   logp    out  float[rows]
+ */
+int ef_token_logp(int64_t rows, int64_t vocab, int type, const void *logits, int64_t stride, const int64_t *tokens,
+                  float *logp, void *stream);
+
+/*
+ * Clipped policy loss with a KL term, and its gradient with respect to the logits.
+ * For row t with token a, logp as above, q = token_weight[t], A = advantage[t]:
+ *     r       = exp(logp - logp_old[t])
+ *     d       = logp_ref[t] - logp
+ *     f       = -min(r * A, clip(r, 1 - clip_low, 1 + clip_high) * A) + kl * (exp(d) - d - 1)
+ *     losses[t] <- q * f,    loss <- sum over rows of losses[t] (added in fp64, ascending order of fixed groups)
+ *     c       = -A * r where r * A <= clip(r) * A, else 0;   c -= kl * (exp(d) - 1)
+ *     dlogits[t][v] <- q * c * ([v = a] - softmax(logits[t])[v])
+ * token_weight carries the mask and the mean (1 / live tokens, 0 for masked ones).  A row of weight 0,
+ * or whose token lies outside [0, vocab), is masked: its logits are not read, its
+ * logp, loss and gradients are 0.
+ *
+ *   logits, tokens  in   as for ef_token_logp
+ *   logp_old  in   float[rows], or NULL: r = 1 (the policy that drew the tokens is the one being trained)
+ *   logp_ref  in   float[rows], or NULL: no KL term
+ *   advantage in   float[rows];  token_weight  in  float[rows], or NULL for ones
+ *   logp      out  float[rows], or NULL
+ *   losses    out  float[rows], or NULL
+ *   loss      out  float, or NULL
+ *   dlogits   out  type[rows][dlogits_stride], or NULL for the loss alone; in place over logits
+ * 0 <= clip_low <= 1, clip_high >= 0, kl >= 0, all finite; one output at least (EF_ERR_NULL).
+ */
+int ef_policy_loss(ef_workspace *workspace, int64_t rows, int64_t vocab, int type, const void *logits, int64_t stride,
+                   const int64_t *tokens, const float *logp_old, const float *logp_ref, const float *advantage,
+                   const float *token_weight, float clip_low, float clip_high, float kl, float *logp, float *losses,
+                   float *loss, void *dlogits, int64_t dlogits_stride, void *stream);
 
 /* Static text for an error code; for EF_ERR_HIP the text of the last HIP error
  * seen by this thread is appended.  The returned pointer stays valid until the

@@ -34,6 +34,9 @@ ABI_SYMBOLS = (
     "ef_plan_set_lazy", "ef_plan_is_lazy", "ef_flush",
     "ef_state_create", "ef_state_destroy", "ef_worker_step_state", "ef_server_step_state", "ef_state_export",
     "ef_state_import",
+    # a worker's forward and backward pass (layers.py)
+    "ef_act_bytes", "ef_act_scales_offset", "ef_act_encode", "ef_act_decode", "ef_norm_forward", "ef_norm_backward",
+    "ef_workspace_create", "ef_workspace_destroy", "ef_weight_grad", "ef_token_logp", "ef_policy_loss",
 )
 # ... and what include/ef_debug.h declares (tuning and diagnostics the tests use)
 DEBUG_SYMBOLS = (
@@ -167,6 +170,7 @@ def lib():
     for name in ("ef_state_export", "ef_state_import"):
         getattr(L, name).restype = c_int
         getattr(L, name).argtypes = [vp, vp, vp, vp, i64, vp, vp]
+    layers.declare(L)
     L.ef_strerror.restype = ctypes.c_char_p
     L.ef_strerror.argtypes = [c_int]
     _load_native(L)
@@ -571,3 +575,9 @@ def ef_state_export(plan, state, mom=None, err=None, server_err=None, stream=Non
 def ef_state_import(plan, state, mom=None, err=None, server_err=None, stream=None):
     """Overwrites the held m, e, e~ with the given finished state (any may be None)."""
     _state_copy(lib().ef_state_import, plan, state, mom, err, server_err, stream)
+
+
+from . import layers  # noqa: E402  (it uses the helpers above)
+from .layers import (EF_NORM_MAX_WIDTH, EF_TYPE_BF16, EF_TYPE_FP32, Workspace, ef_act_bytes, ef_act_decode, ef_act_encode,  # noqa: E402,F401
+                     ef_act_scales_offset, ef_norm_backward, ef_norm_forward, ef_policy_loss, ef_token_logp, ef_weight_grad,
+                     ef_workspace_create, ef_workspace_destroy)

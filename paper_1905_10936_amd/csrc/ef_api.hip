@@ -4,6 +4,7 @@
 #include "ef_debug.h"
 #include "ef_device.h"
 
+#include <algorithm>
 #include <cmath>
 #include <cstdio>
 #include <cstring>
@@ -1657,6 +1658,12 @@ int ef_state_import(const ef_plan *plan, ef_state *state, const float *mom, cons
                       const_cast<float *>(server_err), false, static_cast<hipStream_t>(stream));
 }
 
+}  // extern "C"
+
+#include "ef_layers.h"
+
+extern "C" {
+
 const char *ef_strerror(int code)
 {
     const char *t;
@@ -1665,10 +1672,11 @@ const char *ef_strerror(int code)
     case EF_ERR_NULL: t = "a required pointer is NULL"; break;
     case EF_ERR_OFFSETS: t = "block_offsets is not a partition (0 = o[0] < o[1] < ... < o[B] = d)"; break;
     case EF_ERR_ARG: t = "argument out of range"; break;
-    case EF_ERR_ALIGN: t = "pointer not aligned (fp32 arrays 16 bytes, sign words 8 bytes)"; break;
+    case EF_ERR_ALIGN: t = "pointer not aligned (fp32 arrays 16 bytes, sign words 8 bytes; matrices to their elements, checkpoints 16 bytes)"; break;
     case EF_ERR_SIZE:
         t = "input too large for the static scratch of ef_compressor_quality_static (tiles x vectors above "
-            "EF_QUALITY_STATIC_MAX_TILE_VECTORS): use ef_compressor_quality";
+            "EF_QUALITY_STATIC_MAX_TILE_VECTORS): use ef_compressor_quality; or more rows than a workspace was created for, or wider rows "
+            "than an operator takes";
         break;
     case EF_ERR_HIP:
         snprintf(g_errbuf, sizeof g_errbuf, "HIP runtime error: %s", hipGetErrorString(g_last_hip));

@@ -1,0 +1,227 @@
+// RMS norm with the residual's addition and an 8-bit output, and its backward pass.
+//
+// Both are bound by memory.  A row is held in registers by a team of LANES threads, CHUNKS times eight elements each, and read
+// once: the sum of squares (forward) or of g * xhat (backward) needs the whole row before the first output can be
+// formed.  Teams of up to 64 lanes meet without a barrier.
+#pragma once
+#include "ef_rows.h"
+
+namespace ef {
+
+struct NormForward {
+    int64_t rows, n;
+    const void *x, *residual;
+    int64_t x_stride, residual_stride;
+    const float *weight;
+    float eps;
+    void *h, *y;
+    int64_t h_stride, y_stride;
+    ActRef act;                 // codes == nullptr: none is written
+    float *rstd;
+};
+
+constexpr int norm_threads(int lanes) { return lanes < 256 ? 256 : lanes; }
+
+template <class T, int LANES, int CHUNKS>
+__global__ __launch_bounds__(norm_threads(LANES)) void k_norm_forward(NormForward a)
+{
+    constexpr int TEAMS = norm_threads(LANES) / LANES;
+    __shared__ float sums[LANES > 64 ? LANES / 64 : 1];
+    const int lane = threadIdx.x % LANES;
+    const int64_t row = (int64_t)blockIdx.x * TEAMS + threadIdx.x / LANES;
+    if (row >= a.rows) return;          // whole teams; LANES > 64: never
+    const T *x = static_cast<const T *>(a.x) + row * a.x_stride;
+    float v[CHUNKS][8];
+    {
+        Eight<T> e[CHUNKS];
+#pragma unroll
+        for (int c = 0; c < CHUNKS; ++c) {
+            const int64_t i = (c * LANES + lane) * 8;
+            load_some(e[c], x + i, a.n - i, 0u);
+        }
+        if (a.residual) {
+            const T *r = static_cast<const T *>(a.residual) + row * a.residual_stride;
+            Eight<T> f[CHUNKS];
+#pragma unroll
+            for (int c = 0; c < CHUNKS; ++c) {
+                const int64_t i = (c * LANES + lane) * 8;
+                load_some(f[c], r + i, a.n - i, 0u);
+            }
+#pragma unroll
+            for (int c = 0; c < CHUNKS; ++c)
+#pragma unroll
+                for (int k = 0; k < 8; ++k) v[c][k] = e[c][k] + f[c][k];
+        } else {
+#pragma unroll
+            for (int c = 0; c < CHUNKS; ++c)
+#pragma unroll
+                for (int k = 0; k < 8; ++k) v[c][k] = e[c][k];
+        }
+    }
+    float s = 0.0f;
+#pragma unroll
+    for (int c = 0; c < CHUNKS; ++c)
+#pragma unroll
+        for (int k = 0; k < 8; ++k) s = __builtin_fmaf(v[c][k], v[c][k], s);
+    s = over_row<Add, LANES>(s, sums);
+    const float rstd = 1.0f / sqrtf(s / (float)a.n + a.eps);
+    if (a.rstd && lane == 0) a.rstd[row] = rstd;
+    if (a.h) {
+        T *h = static_cast<T *>(a.h) + row * a.h_stride;
+#pragma unroll
+        for (int c = 0; c < CHUNKS; ++c) {
+            const int64_t i = (c * LANES + lane) * 8;
+            Eight<T> e;
+            e.round(v[c]);
+            store_some(e, h + i, a.n - i);
+        }
+    }
+#pragma unroll
+    for (int c = 0; c < CHUNKS; ++c)
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[c][k] *= rstd;
+    if (a.act.codes) {
+#pragma unroll
+        for (int c = 0; c < CHUNKS; ++c) a.act.put(row, (c * LANES + lane) * 8, a.n, v[c]);
+    }
+    if (a.y) {
+        T *y = static_cast<T *>(a.y) + row * a.y_stride;
+#pragma unroll
+        for (int c = 0; c < CHUNKS; ++c) {
+            const int64_t i = (c * LANES + lane) * 8;
+            if (a.weight) {
+                Eight<float> w;
+                load_some(w, a.weight + i, a.n - i, 0u);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) v[c][k] *= w[k];
+            }
+            Eight<T> e;
+            e.round(v[c]);
+            store_some(e, y + i, a.n - i);
+        }
+    }
+}
+
+struct NormBackward {
+    int64_t rows, n;
+    const void *dy, *dh;
+    int64_t dy_stride, dh_stride;
+    ActRef act;
+    const float *rstd, *weight;
+    void *dx;
+    int64_t dx_stride;
+    float *parts;               // [workgroups][n] sums of dy * xhat over each workgroup's rows, or NULL
+};
+
+// A team takes rows team, team + teams, ... and keeps its sums of dy * xhat in registers; a workgroup's teams add theirs up in shared
+// memory, one after the other, so that the order is fixed.
+template <class T, int LANES, int CHUNKS>
+__global__ __launch_bounds__(norm_threads(LANES)) void k_norm_backward(NormBackward a)
+{
+    constexpr int TEAMS = norm_threads(LANES) / LANES;
+    __shared__ float sums[2][LANES > 64 ? LANES / 64 : 1];
+    __shared__ float joined[TEAMS > 1 ? LANES * CHUNKS * 8 : 1];
+    const int lane = threadIdx.x % LANES, team = threadIdx.x / LANES;
+    float dw[CHUNKS][8], w[CHUNKS][8];
+#pragma unroll
+    for (int c = 0; c < CHUNKS; ++c) {
+        const int64_t i = (c * LANES + lane) * 8;
+        Eight<float> e;
+        if (a.weight)
+            load_some(e, a.weight + i, a.n - i, 0u);
+        else
+            e.fill(0x3f800000u);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            w[c][k] = e[k];
+            dw[c][k] = 0.0f;
+        }
+    }
+    const float per = 1.0f / (float)a.n;
+    int turn = 0;
+    for (int64_t row = (int64_t)blockIdx.x * TEAMS + team; row < a.rows; row += (int64_t)gridDim.x * TEAMS) {
+        const T *dy = static_cast<const T *>(a.dy) + row * a.dy_stride;
+        Eight<T> e[CHUNKS], f[CHUNKS];
+        float x[CHUNKS][8];
+#pragma unroll
+        for (int c = 0; c < CHUNKS; ++c) {
+            const int64_t i = (c * LANES + lane) * 8;
+            load_some(e[c], dy + i, a.n - i, 0u);
+            if (a.dh) load_some(f[c], static_cast<const T *>(a.dh) + row * a.dh_stride + i, a.n - i, 0u);
+            a.act.get(row, i, x[c]);
+        }
+        const float rstd = a.rstd[row];
+        float s = 0.0f;
+#pragma unroll
+        for (int c = 0; c < CHUNKS; ++c)
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const float d = e[c][k];
+                dw[c][k] = __builtin_fmaf(d, x[c][k], dw[c][k]);
+                s = __builtin_fmaf(d * w[c][k], x[c][k], s);
+            }
+        s = over_row<Add, LANES>(s, sums[turn & 1]) * per;
+        ++turn;
+        T *dx = static_cast<T *>(a.dx) + row * a.dx_stride;
+#pragma unroll
+        for (int c = 0; c < CHUNKS; ++c) {
+            const int64_t i = (c * LANES + lane) * 8;
+            float v[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                v[k] = rstd * __builtin_fmaf(-s, x[c][k], e[c][k] * w[c][k]);
+                if (a.dh) v[k] += f[c][k];
+            }
+            Eight<T> o;
+            o.round(v);
+            store_some(o, dx + i, a.n - i);
+        }
+    }
+    if (!a.parts) return;
+    float *part = a.parts + (int64_t)blockIdx.x * a.n;
+    if constexpr (TEAMS > 1) {
+        for (int t = 0; t < TEAMS; ++t) {
+            if (t == team) {
+#pragma unroll
+                for (int c = 0; c < CHUNKS; ++c)
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) {
+                        float *j = &joined[(c * 8 + k) * LANES + lane];
+                        *j = t ? *j + dw[c][k] : dw[c][k];
+                    }
+            }
+            __syncthreads();
+        }
+        for (int i = threadIdx.x; i < LANES * CHUNKS * 8; i += blockDim.x) {
+            const int l = i / 8 % LANES, c = i / 8 / LANES, k = i % 8;
+            if (i < a.n) part[i] = joined[(c * 8 + k) * LANES + l];
+        }
+    } else {
+#pragma unroll
+        for (int c = 0; c < CHUNKS; ++c) {
+            const int64_t i = (c * LANES + lane) * 8;
+            Eight<float> e;
+            e.round(dw[c]);
+            store_some(e, part + i, a.n - i);
+        }
+    }
+}
+
+// dweight <- [dweight +] the sum of `count` partial rows: 64 columns to a workgroup, its four wavefronts take every fourth row.
+__global__ __launch_bounds__(256) void k_sum_parts(const float *parts, int count, int64_t n, float *dweight, int accumulate)
+{
+    __shared__ float sums[4][64];
+    const int64_t i = (int64_t)blockIdx.x * 64 + threadIdx.x % 64;
+    const int wave = threadIdx.x / 64;
+    float s = 0.0f;
+    if (i < n)
+        for (int p = wave; p < count; p += 4) s += parts[(int64_t)p * n + i];
+    sums[wave][threadIdx.x % 64] = s;
+    __syncthreads();
+    if (wave == 0 && i < n) {
+        s = (sums[0][threadIdx.x] + sums[1][threadIdx.x]) + (sums[2][threadIdx.x] + sums[3][threadIdx.x]);
+        dweight[i] = accumulate ? dweight[i] + s : s;
+    }
+}
+
+}  // namespace ef
