@@ -56,64 +56,56 @@ __device__ __forceinline__ ThreeParts three_parts(float v)
     return p;
 }
 
-// What a thread carries from memory to LDS for one step.
+// What a thread carries from memory to LDS for one step.  Nothing is masked: channels past the operands' ends hold whatever lies there, and
+// what they give is not stored.  Steps whose reads could pass the end of dz are filled in by fill() instead.
 template <class T>
 struct GradStage {
     static constexpr int TOKENS = GradStep<T>::TOKENS, PARTS = GradStep<T>::PARTS;
     static constexpr int Z = TOKENS * GRAD_TILE * (int)sizeof(T) / 16 / GRAD_THREADS;   // 128-bit words of dz: 8
     static constexpr int X = TOKENS * GRAD_TILE / 16 / GRAD_THREADS;                    // of codes: 4 or 2
-    u32x4 z[Z], x[X];
-    unsigned s[X];
-
     static constexpr int Z_WORDS = GRAD_TILE * (int)sizeof(T) / 16;     // words a token
     static constexpr int Z_ELEMS = 16 / (int)sizeof(T);
+    u32x4 z[Z], x[X];
+    unsigned s[X];
+    // This thread's first words of the step to load next, in global memory: a load that might be LDS's would have every LDS read waited for.
+    const EF_GLOBAL T *z_from;
+    const EF_GLOBAL uint8_t *x_from, *s_from;
 
-    __device__ __forceinline__ void load(const GradArgs &a, int64_t token0, int64_t o0, int64_t n0)
+    __device__ __forceinline__ void begin(const GradArgs &a, int64_t token0, int64_t o0, int64_t n0)
     {
         const int tid = threadIdx.x;
-        const int64_t o = o0 + tid % Z_WORDS * Z_ELEMS;
-#pragma unroll
-        for (int k = 0; k < Z; ++k) {
-            const int64_t t = token0 + tid / Z_WORDS + k * (GRAD_THREADS / Z_WORDS);
-            const T *p = static_cast<const T *>(a.dz) + t * a.dz_stride + o;
-            z[k] = u32x4{0, 0, 0, 0};
-            if (t < a.rows) {
-                if (o + Z_ELEMS <= a.out) {
-                    if constexpr (sizeof(T) == 2)
-                        z[k] = *reinterpret_cast<const u32x4_any *>(p);
-                    else
-                        z[k] = *reinterpret_cast<const u32x4_word *>(p);
-                } else {
-#pragma unroll
-                    for (int i = 0; i < Z_ELEMS - 1; ++i)
-                        if (o + i < a.out) {
-                            const unsigned b = element_bits(p + i);
-                            if constexpr (sizeof(T) == 2)
-                                z[k][i / 2] |= i & 1 ? b << 16 : b;
-                            else
-                                z[k][i] = b;
-                        }
-                }
-            }
-        }
-        const int64_t i = n0 + tid % 16 * 16;
-#pragma unroll
-        for (int k = 0; k < X; ++k) {
-            const int64_t t = token0 + tid / 16 + k * (GRAD_THREADS / 16);
-            x[k] = u32x4{0, 0, 0, 0};
-            s[k] = SCALE_MIN;
-            if (t < a.rows && i < a.act.groups * GROUP) {
-                x[k] = *reinterpret_cast<const u32x4 *>(a.act.code_at(t, i));
-                s[k] = *a.act.scale_at(t, i);
-            }
+        int64_t o = o0 + tid % Z_WORDS * Z_ELEMS, i = n0 + tid % 16 * 16;
+        if (o >= a.out) o = 0;
+        if (i >= a.act.groups * GROUP) i = 0;
+        z_from = (const EF_GLOBAL T *)(static_cast<const T *>(a.dz) + (token0 + tid / Z_WORDS) * a.dz_stride + o);
+        x_from = (const EF_GLOBAL uint8_t *)a.act.code_at(token0 + tid / 16, i);
+        s_from = (const EF_GLOBAL uint8_t *)a.act.scale_at(token0 + tid / 16, i);
+    }
+    // Word k of dz (k < Z) or of the codes (k - Z); next() goes on to the following step.
+    __device__ __forceinline__ void load(const GradArgs &a, int k)
+    {
+        if (k < Z) {
+            const EF_GLOBAL T *p = z_from + (int64_t)k * (GRAD_THREADS / Z_WORDS) * a.dz_stride;
+            if constexpr (sizeof(T) == 2)
+                z[k] = *(const EF_GLOBAL u32x4_any *)p;
+            else
+                z[k] = *(const EF_GLOBAL u32x4_word *)p;
+        } else {
+            k -= Z;
+            x[k] = *(const EF_GLOBAL u32x4 *)(x_from + k * (GRAD_THREADS / 16) * a.act.groups * GROUP);
+            s[k] = s_from[k * (GRAD_THREADS / 16) * a.act.groups];
         }
     }
-
-    __device__ __forceinline__ void store(char *buffer) const
+    __device__ __forceinline__ void next(const GradArgs &a)
+    {
+        z_from += TOKENS * a.dz_stride;
+        x_from += TOKENS * a.act.groups * GROUP;
+        s_from += TOKENS * a.act.groups;
+    }
+    __device__ __forceinline__ void store(char *buffer, int k) const
     {
         const int tid = threadIdx.x;
-#pragma unroll
-        for (int k = 0; k < Z; ++k) {
+        if (k < Z) {
             const int t = tid / Z_WORDS + k * (GRAD_THREADS / Z_WORDS);
             if constexpr (sizeof(T) == 2) {
                 *reinterpret_cast<u32x4 *>(buffer + t * GRAD_PITCH + tid % Z_WORDS * 16) = z[k];
@@ -126,21 +118,42 @@ struct GradStage {
                 *reinterpret_cast<u32x2 *>(at + TOKENS * GRAD_PITCH) = u32x2{p[0].b >> 16 | p[1].b, p[2].b >> 16 | p[3].b};
                 *reinterpret_cast<u32x2 *>(at + 2 * TOKENS * GRAD_PITCH) = u32x2{p[0].c >> 16 | p[1].c, p[2].c >> 16 | p[3].c};
             }
-        }
-        char *const xs = buffer + PARTS * TOKENS * GRAD_PITCH;
-#pragma unroll
-        for (int k = 0; k < X; ++k) {
+        } else {
+            k -= Z;
             const int t = tid / 16 + k * (GRAD_THREADS / 16);
             const float scale = scale_value(s[k]);
-            u32x4 w[2];
+            char *at = buffer + (PARTS * TOKENS + t) * GRAD_PITCH + tid % 16 * 32;
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 const u32x2 lo = decode_four(x[k][2 * h], scale), hi = decode_four(x[k][2 * h + 1], scale);
-                w[h] = u32x4{lo.x, lo.y, hi.x, hi.y};
+                *reinterpret_cast<u32x4 *>(at + 16 * h) = u32x4{lo.x, lo.y, hi.x, hi.y};
             }
-            char *at = xs + t * GRAD_PITCH + tid % 16 * 32;
-            *reinterpret_cast<u32x4 *>(at) = w[0];
-            *reinterpret_cast<u32x4 *>(at + 16) = w[1];
+        }
+    }
+
+    // The same for the step at token0, element by element and nothing read that is not there; zeros in its place.
+    static __device__ void fill(const GradArgs &a, int64_t token0, int64_t o0, int64_t n0, char *buffer)
+    {
+        for (int k = threadIdx.x; k < TOKENS * GRAD_TILE; k += GRAD_THREADS) {
+            const int t = k / GRAD_TILE, c = k % GRAD_TILE;
+            const bool there = token0 + t < a.rows;
+            char *at = buffer + t * GRAD_PITCH + c * 2;
+            unsigned v = 0;
+            if (there && o0 + c < a.out) v = element_bits(static_cast<const T *>(a.dz) + (token0 + t) * a.dz_stride + o0 + c);
+            if constexpr (sizeof(T) == 2) {
+                *reinterpret_cast<uint16_t *>(at) = (uint16_t)v;
+            } else {
+                const ThreeParts p = three_parts(__uint_as_float(v));
+                *reinterpret_cast<uint16_t *>(at) = (uint16_t)(p.a >> 16);
+                *reinterpret_cast<uint16_t *>(at + TOKENS * GRAD_PITCH) = (uint16_t)(p.b >> 16);
+                *reinterpret_cast<uint16_t *>(at + 2 * TOKENS * GRAD_PITCH) = (uint16_t)(p.c >> 16);
+            }
+            uint16_t x = 0;
+            if (there && n0 + c < a.n) {
+                const unsigned code = *a.act.code_at(token0 + t, n0 + c), scale = *a.act.scale_at(token0 + t, n0 + c);
+                x = (uint16_t)decode_four(code, scale_value(scale)).x;
+            }
+            *reinterpret_cast<uint16_t *>(buffer + (PARTS * TOKENS + t) * GRAD_PITCH + c * 2) = x;
         }
     }
 };
@@ -189,40 +202,93 @@ __global__ __launch_bounds__(GRAD_THREADS, 1) void k_weight_grad(GradArgs a)
 #pragma unroll
             for (int k = 0; k < 16; ++k) acc[i][j][k] = 0.0f;
 
-    if (first < last) {
-        GradStage<T> stage;
-        stage.load(a, first * TOKENS, o0, n0);
-        stage.store(buffers[0]);
-        stage.load(a, (first + 1) * TOKENS, o0, n0);        // past the last token: zeros, nothing is read
-        __syncthreads();
-        for (int64_t step = first; step < last; ++step) {
-            const char *now = buffers[(step - first) & 1];
-            if (step + 1 < last) {
-                stage.store(buffers[(step - first + 1) & 1]);
-                stage.load(a, (step + 2) * TOKENS, o0, n0);
-            }
+    // Steps before `safe` read nothing past dz's end: a token's last word may reach seven elements past its row.
+    const int64_t spare = o0 + GRAD_TILE <= a.out ? 0 : (7 + a.dz_stride - 1) / a.dz_stride;
+    const int64_t safe = min(last, (a.rows - spare) / TOKENS);
+    constexpr int REGIONS = TOKENS / 16 * PARTS, WORDS = GradStage<T>::Z + GradStage<T>::X;
+    bf16x8 z[2][4], x[2][4];
+    // fragment f of region r: x's where a region begins with another sixteen tokens, then dz's
+    auto fragment = [&](const char *buffer, int r, int f) {
+        const int k = r / PARTS, p = r % PARTS;
+        if (f < 4) {
+            if (p == 0) x[k & 1][f] = read_transposed(buffer + x_at + k * 16 * GRAD_PITCH + f * 64);
+        } else {
+            z[r & 1][f - 4] = read_transposed(buffer + z_at + (p * TOKENS + k * 16) * GRAD_PITCH + (f - 4) * 64);
+        }
+    };
+    auto product = [&](int r, int i, int j) {
+        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(z[r & 1][i], x[r / PARTS & 1][j], acc[i][j], 0, 0, 0);
+    };
+    int64_t step = first;
+    char *now = buffers[0], *next = buffers[1];
+    GradStage<T> stage;
+    stage.begin(a, first * TOKENS, o0, n0);
+    if (first < safe) {
 #pragma unroll
-            for (int k = 0; k < TOKENS / 16; ++k) {
-                bf16x8 x[4];
+        for (int k = 0; k < WORDS; ++k) stage.load(a, k);
+        if (first + 1 < safe) stage.next(a);
 #pragma unroll
-                for (int j = 0; j < 4; ++j) x[j] = read_transposed(now + x_at + k * 16 * GRAD_PITCH + j * 64);
+        for (int k = 0; k < WORDS; ++k) {
+            stage.store(now, k);
+            stage.load(a, k);
+        }
+        if (first + 2 < safe) stage.next(a);
+    } else if (first < last) {
+        GradStage<T>::fill(a, first * TOKENS, o0, n0, now);
+    }
+    __syncthreads();
+    if (step + 1 < safe) {
 #pragma unroll
-                for (int p = 0; p < PARTS; ++p) {
-                    bf16x8 z[4];
+        for (int f = 0; f < 8; ++f) fragment(now, 0, f);
+        for (; step + 1 < safe; ++step) {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) z[i] = read_transposed(now + z_at + (p * TOKENS + k * 16) * GRAD_PITCH + i * 64);
+            for (int r = 0; r < REGIONS; ++r) {
+                if (r == REGIONS - 1) __syncthreads();
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(z[i], x[j], acc[i][j], 0, 0, 0);
+                for (int m = 0; m < 16; ++m) {
+                    product(r, m / 4, m % 4);
+                    if (m < 8) {
+                        if (r < REGIONS - 1)
+                            fragment(now, r + 1, m);
+                        else
+                            fragment(next, 0, m);
+                    } else if (r < REGIONS - 1) {
+                        // words of the next step to LDS, those of the one behind it on their way into the same registers
+                        constexpr int EACH = (WORDS + REGIONS - 2) / (REGIONS - 1);
+                        const int w = r * EACH + (m - 8) / 2;
+                        if (m % 2 == 0 && (m - 8) / 2 < EACH && w < WORDS) {
+                            stage.store(next, w);
+                            stage.load(a, w);
+                        }
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
                 }
             }
-            __syncthreads();
+            if (step + 3 < safe) stage.next(a);
+            char *t = now;
+            now = next;
+            next = t;
         }
     }
+    for (; step < last; ++step) {
+        if (step + 1 < last) GradStage<T>::fill(a, (step + 1) * TOKENS, o0, n0, next);
+#pragma unroll
+        for (int r = 0; r < REGIONS; ++r) {
+#pragma unroll
+            for (int f = 0; f < 8; ++f) fragment(now, r, f);
+#pragma unroll
+            for (int m = 0; m < 16; ++m) product(r, m / 4, m % 4);
+        }
+        __syncthreads();
+        char *t = now;
+        now = next;
+        next = t;
+    }
 
-    float *dw = a.dw + (a.splits > 1 ? (int64_t)split * a.out * a.n : 0);
+    // An accumulator's lane holds channel lane % 32 of x's side and four runs of four of dz's.
+    float *const dw = a.dw + (a.splits > 1 ? (int64_t)split * a.out * a.n : 0) + (o0 + wave / 2 * 128 + 4 * (lane / 32)) * a.n;
     const bool whole = a.splits == 1;
+    const int64_t left = a.out - (o0 + wave / 2 * 128 + 4 * (lane / 32));
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         const int64_t i = n0 + wave % 2 * 128 + j * 32 + lane % 32;
@@ -230,16 +296,20 @@ __global__ __launch_bounds__(GRAD_THREADS, 1) void k_weight_grad(GradArgs a)
         const float s = whole && a.scale ? a.scale[i] : 1.0f;
 #pragma unroll
         for (int m = 0; m < 4; ++m) {
+            float v[16];
 #pragma unroll
-            for (int k = 0; k < 16; ++k) {
-                const int64_t o = o0 + wave / 2 * 128 + m * 32 + 8 * (k / 4) + 4 * (lane / 32) + k % 4;
-                if (o < a.out) {
-                    float *at = dw + o * a.n + i;
-                    float v = acc[m][j][k] * s;
-                    if (whole && a.accumulate) v += *at;
-                    *at = v;
-                }
+            for (int k = 0; k < 16; ++k) v[k] = acc[m][j][k] * s;
+            float *const at = dw + m * 32 * a.n + i;
+            if (whole && a.accumulate) {
+                float old[16];
+#pragma unroll
+                for (int k = 0; k < 16; ++k) old[k] = m * 32 + 8 * (k / 4) + k % 4 < left ? at[(8 * (k / 4) + k % 4) * a.n] : 0.0f;
+#pragma unroll
+                for (int k = 0; k < 16; ++k) v[k] += old[k];
             }
+#pragma unroll
+            for (int k = 0; k < 16; ++k)
+                if (m * 32 + 8 * (k / 4) + k % 4 < left) at[(8 * (k / 4) + k % 4) * a.n] = v[k];
         }
     }
 }

@@ -312,7 +312,7 @@ int ef_norm_backward(ef_workspace *workspace, int64_t rows, int64_t width, int t
         EF_HIP(hipGetLastError());
     }
     if (dweight) {
-        hipLaunchKernelGGL(ef::k_sum_parts, dim3((unsigned)ceil_div(width, 64)), dim3(256), 0, s, workspace->parts, groups, width, dweight,
+        hipLaunchKernelGGL(ef::k_sum_parts, dim3((unsigned)ceil_div(width, 32)), dim3(1024), 0, s, workspace->parts, groups, width, dweight,
                            accumulate ? 1 : 0);
         EF_HIP(hipGetLastError());
     }

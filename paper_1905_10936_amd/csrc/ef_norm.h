@@ -207,19 +207,29 @@ __global__ __launch_bounds__(norm_threads(LANES)) void k_norm_backward(NormBackw
     }
 }
 
-// dweight <- [dweight +] the sum of `count` partial rows: 64 columns to a workgroup, its four wavefronts take every fourth row.
-__global__ __launch_bounds__(256) void k_sum_parts(const float *parts, int count, int64_t n, float *dweight, int accumulate)
+// dweight <- [dweight +] the sum of `count` partial rows: 32 columns to a workgroup, whose 32 half wavefronts take every 32nd row, up to sixteen of
+// them on their way at once, and add their sums up in order.
+__global__ __launch_bounds__(1024) void k_sum_parts(const float *parts, int count, int64_t n, float *dweight, int accumulate)
 {
-    __shared__ float sums[4][64];
-    const int64_t i = (int64_t)blockIdx.x * 64 + threadIdx.x % 64;
-    const int wave = threadIdx.x / 64;
+    __shared__ float sums[32][33];
+    const int col = threadIdx.x % 32, first = threadIdx.x / 32;
+    const int64_t i = (int64_t)blockIdx.x * 32 + col;
     float s = 0.0f;
-    if (i < n)
-        for (int p = wave; p < count; p += 4) s += parts[(int64_t)p * n + i];
-    sums[wave][threadIdx.x % 64] = s;
+    if (i < n) {
+        for (int p = first; p < count; p += 16 * 32) {
+            float v[16];
+#pragma unroll
+            for (int k = 0; k < 16; ++k) v[k] = p + k * 32 < count ? parts[(int64_t)(p + k * 32) * n + i] : 0.0f;
+#pragma unroll
+            for (int k = 0; k < 16; ++k) s += v[k];
+        }
+    }
+    sums[first][col] = s;
     __syncthreads();
-    if (wave == 0 && i < n) {
-        s = (sums[0][threadIdx.x] + sums[1][threadIdx.x]) + (sums[2][threadIdx.x] + sums[3][threadIdx.x]);
+    if (first == 0 && i < n) {
+        s = 0.0f;
+#pragma unroll
+        for (int k = 0; k < 32; ++k) s += sums[k][col];
         dweight[i] = accumulate ? dweight[i] + s : s;
     }
 }

@@ -10,6 +10,8 @@
 
 namespace ef {
 
+#define EF_GLOBAL __attribute__((address_space(1)))
+
 constexpr int GROUP = 32;       // elements to a scale
 
 struct bf16_t { uint16_t bits; };
