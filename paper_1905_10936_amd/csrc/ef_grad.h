@@ -3,38 +3,26 @@
 // What a checkpoint stands for is a bf16 number exactly (the scales are powers of two), so the product runs on bf16 matrix
 // instructions with nothing lost but fp32's own rounding of the sums; an fp32 gradient enters as three bf16 numbers, which are its 24 bits.
 //
-// A workgroup of four wavefronts makes a tile of 256 x 256 of dw, 128 x 128 to a wavefront in 256 accumulators a lane: per product
-// step of 16 tokens a wavefront reads 8 KiB from LDS for 16 instructions of 32 cycles, 64 of the 128 bytes a cycle that LDS gives.
-// Both operands lie in memory with the tokens as the slow index, and the instruction wants eight tokens of one channel in a lane: the
-// tiles are kept in LDS as they lie in memory and read transposed (four tokens by 16 channels to a read).  Rows of a tile are
-// 576 bytes apart, so that the four tokens of two neighbouring reads fall on different banks.
+// A workgroup of four wavefronts makes a square tile of dw of 64 SIDE channels, a quarter each: with SIDE = 4 256 x 256, 256 accumulators a lane.
+// Both operands lie in memory with the tokens as the slow index, and the instruction wants eight tokens of one channel in a lane: the tiles
+// are kept in LDS as they lie in memory, codes already decoded, and read transposed (four tokens by 16 channels to a read).  From a token's channels to
+// the next token's are 64 bytes more than they take, so that the four tokens of a read fall on different banks.
 #pragma once
 #include "ef_rows.h"
+
+#include <type_traits>
+#include <utility>
 
 namespace ef {
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 constexpr int GRAD_THREADS = 256;
-constexpr int GRAD_TILE = 256;          // channels of either side
-constexpr int GRAD_PITCH = 576;         // bytes from a token's channels to the next one's in LDS
-constexpr int GRAD_ROWS = 128;          // such rows in a buffer: dz's, then x's
+constexpr int GRAD_ROWS = 128;          // tokens' rows in an LDS buffer: dz's (three to a token in fp32), then x's
 
-struct GradArgs {
-    int64_t rows, out, n;
-    const void *dz;
-    int64_t dz_stride;
-    ActRef act;
-    const float *scale;
-    float *dw;                          // or the partial results, [splits][out][n]
-    int accumulate;
-    int tiles_out, tiles_n;
-    int splits;
-    int64_t steps;                      // product steps in all; a split takes an equal share of them
-};
-
-// Tokens in a step: dz takes one row of LDS a token in bf16 and three in fp32.
+// Tokens in a step, bf16 parts of an element of dz.
 template <class T>
 struct GradStep;
 template <>
@@ -42,289 +30,450 @@ struct GradStep<bf16_t> { static constexpr int TOKENS = 64, PARTS = 1; };
 template <>
 struct GradStep<float> { static constexpr int TOKENS = 32, PARTS = 3; };
 
-// The three bf16 numbers whose sum a finite fp32 number is, each cut off, not rounded; an infinity is its own first part.
-struct ThreeParts { unsigned a, b, c; };        // in the upper halves
-__device__ __forceinline__ ThreeParts three_parts(float v)
-{
-    ThreeParts p;
-    p.a = __float_as_uint(v) & 0xffff0000u;
-    float rest = v - __uint_as_float(p.a);
-    if (__float_as_uint(v) << 1 == 0xff000000u) rest = 0.0f;
-    p.b = __float_as_uint(rest) & 0xffff0000u;
-    rest -= __uint_as_float(p.b);
-    p.c = __float_as_uint(rest) & 0xffff0000u;
-    return p;
-}
+struct GradArgs {
+    int64_t rows, out, n;
+    const void *dz;
+    int64_t dz_stride;
+    ActRef act;
+    const float *scale;
+    float *dw;
+    int accumulate;
+    int tiles, tiles_n;                 // in all, and in a row of them
+    // The last tiles, from `whole` on, are cut into `splits` parts along the tokens, a workgroup each; their sums go to `parts`, tile by tile, and
+    // k_join_splits adds them up.
+    int whole, splits;
+    float *parts;
+    int64_t steps;                      // of the tokens
+};
 
-// What a thread carries from memory to LDS for one step.  Nothing is masked: channels past the operands' ends hold whatever lies there, and
-// what they give is not stored.  Steps whose reads could pass the end of dz are filled in by fill() instead.
-template <class T>
+// An fp32 number is the sum of three bf16 ones: its upper half, that of what is left, and the rest, each cut off, not rounded.  Of an infinity or NaN
+// nothing is left (fmaxf takes a number over NaN).
+__device__ __forceinline__ float upper(float v) { return __uint_as_float(__float_as_uint(v) & 0xffff0000u); }
+__device__ __forceinline__ float cut_off(float v) { return copysignf(fmaxf(fabsf(v - upper(v)), 0.0f), v); }
+__device__ __forceinline__ unsigned uppers(unsigned lo, unsigned hi) { return __builtin_amdgcn_perm(hi, lo, 0x07060302u); }
+
+// What a thread carries from memory to LDS for one step.  load() masks nothing: channels past the operands' ends hold whatever lies there, and what they
+// give is not stored; steps whose reads could pass the end of dz are loaded by load_guarded().
+template <class T, int SIDE>
 struct GradStage {
-    static constexpr int TOKENS = GradStep<T>::TOKENS, PARTS = GradStep<T>::PARTS;
-    static constexpr int Z = TOKENS * GRAD_TILE * (int)sizeof(T) / 16 / GRAD_THREADS;   // 128-bit words of dz: 8
-    static constexpr int X = TOKENS * GRAD_TILE / 16 / GRAD_THREADS;                    // of codes: 4 or 2
-    static constexpr int Z_WORDS = GRAD_TILE * (int)sizeof(T) / 16;     // words a token
-    static constexpr int Z_ELEMS = 16 / (int)sizeof(T);
-    u32x4 z[Z], x[X];
-    unsigned s[X];
-    // This thread's first words of the step to load next, in global memory: a load that might be LDS's would have every LDS read waited for.
-    const EF_GLOBAL T *z_from;
-    const EF_GLOBAL uint8_t *x_from, *s_from;
+    // Steps on their way at a time: a step of a small tile takes less than its loads.
+    static constexpr int DEPTH = SIDE == 4 ? 1 : (SIDE == 2 ? 2 : 3);
+    static constexpr int TOKENS = GradStep<T>::TOKENS, PARTS = GradStep<T>::PARTS, TILE = 64 * SIDE, PITCH = TILE * 2 + 64;
+    static constexpr int Z_ELEMS = 16 / (int)sizeof(T), Z_WORDS = TILE / Z_ELEMS, Z_ROWS = GRAD_THREADS / Z_WORDS, Z = TOKENS / Z_ROWS;
+    static constexpr int X_WORDS = TILE / 16, X_ROWS = GRAD_THREADS / X_WORDS < TOKENS ? GRAD_THREADS / X_WORDS : TOKENS, X = TOKENS / X_ROWS;
+    u32x4 z[DEPTH][Z], x[DEPTH][X];
+    unsigned s[DEPTH][X];
+    // Where the step to load next begins, the same for the whole workgroup, and this thread's bytes from there.  In global memory: a load that
+    // might be LDS's would have every LDS read waited for.
+    const EF_GLOBAL char *z_base;
+    const EF_GLOBAL uint8_t *x_base, *s_base;
+    unsigned z_off, x_off, s_off;
+
+    // the thread's place in a step's words of dz and of codes (threads beyond X_ROWS rows of codes do what others do)
+    static __device__ __forceinline__ int z_row() { return threadIdx.x / Z_WORDS; }
+    static __device__ __forceinline__ int x_row() { return threadIdx.x / X_WORDS % X_ROWS; }
+    static __device__ __forceinline__ int z_word() { return threadIdx.x % Z_WORDS; }
+    static __device__ __forceinline__ int x_word() { return threadIdx.x % X_WORDS; }
 
     __device__ __forceinline__ void begin(const GradArgs &a, int64_t token0, int64_t o0, int64_t n0)
     {
-        const int tid = threadIdx.x;
-        int64_t o = o0 + tid % Z_WORDS * Z_ELEMS, i = n0 + tid % 16 * 16;
-        if (o >= a.out) o = 0;
-        if (i >= a.act.groups * GROUP) i = 0;
-        z_from = (const EF_GLOBAL T *)(static_cast<const T *>(a.dz) + (token0 + tid / Z_WORDS) * a.dz_stride + o);
-        x_from = (const EF_GLOBAL uint8_t *)a.act.code_at(token0 + tid / 16, i);
-        s_from = (const EF_GLOBAL uint8_t *)a.act.scale_at(token0 + tid / 16, i);
+        const int64_t o = o0 + z_word() * Z_ELEMS, i = n0 + x_word() * 16;
+        z_base = (const EF_GLOBAL char *)a.dz + token0 * a.dz_stride * (int64_t)sizeof(T);
+        x_base = (const EF_GLOBAL uint8_t *)a.act.code_at(token0, 0);
+        s_base = (const EF_GLOBAL uint8_t *)a.act.scale_at(token0, 0);
+        // channels past the ends are read from the first ones
+        z_off = (unsigned)((z_row() * a.dz_stride + (o < a.out ? o : 0)) * (int64_t)sizeof(T));
+        x_off = (unsigned)(x_row() * a.act.groups * GROUP + (i < a.act.groups * GROUP ? i : 0));
+        s_off = (unsigned)(x_row() * a.act.groups + (i < a.act.groups * GROUP ? i / GROUP : 0));
     }
-    // Word k of dz (k < Z) or of the codes (k - Z); next() goes on to the following step.
-    __device__ __forceinline__ void load(const GradArgs &a, int k)
+    // The first step that load() may not take: a token's last word may reach Z_ELEMS - 1 elements past its row, and the offsets have to fit 32 bits.
+    static __device__ __forceinline__ int64_t unsafe(const GradArgs &a, int64_t o0)
     {
-        if (k < Z) {
-            const EF_GLOBAL T *p = z_from + (int64_t)k * (GRAD_THREADS / Z_WORDS) * a.dz_stride;
-            if constexpr (sizeof(T) == 2)
-                z[k] = *(const EF_GLOBAL u32x4_any *)p;
-            else
-                z[k] = *(const EF_GLOBAL u32x4_word *)p;
-        } else {
-            k -= Z;
-            x[k] = *(const EF_GLOBAL u32x4 *)(x_from + k * (GRAD_THREADS / 16) * a.act.groups * GROUP);
-            s[k] = s_from[k * (GRAD_THREADS / 16) * a.act.groups];
-        }
+        if (a.dz_stride > (int64_t)1 << 26) return 0;
+        const int64_t spare = o0 + TILE <= a.out ? 0 : (Z_ELEMS - 1 + a.dz_stride - 1) / a.dz_stride;
+        return max((int64_t)0, a.rows - spare) / TOKENS;
+    }
+    // An offset that is 32 bits wide where it is used: the load then adds it to a scalar base itself.
+    static __device__ __forceinline__ unsigned here(unsigned off)
+    {
+        asm volatile("" : "+v"(off));
+        return off;
+    }
+    __device__ __forceinline__ void load_z(const GradArgs &a, int d, int k)
+    {
+        const EF_GLOBAL char *p = z_base + (int64_t)k * Z_ROWS * a.dz_stride * (int64_t)sizeof(T) + here(z_off);
+        if constexpr (sizeof(T) == 2)
+            z[d][k] = *(const EF_GLOBAL u32x4_any *)p;
+        else
+            z[d][k] = *(const EF_GLOBAL u32x4_word *)p;
+    }
+    __device__ __forceinline__ void load_x(const GradArgs &a, int d, int k)
+    {
+        x[d][k] = *(const EF_GLOBAL u32x4 *)(x_base + k * X_ROWS * a.act.groups * GROUP + here(x_off));
+        s[d][k] = *(s_base + k * X_ROWS * a.act.groups + here(s_off));
+    }
+    __device__ __forceinline__ void load(const GradArgs &a, int d)
+    {
+#pragma unroll
+        for (int k = 0; k < Z; ++k) load_z(a, d, k);
+#pragma unroll
+        for (int k = 0; k < X; ++k) load_x(a, d, k);
     }
     __device__ __forceinline__ void next(const GradArgs &a)
     {
-        z_from += TOKENS * a.dz_stride;
-        x_from += TOKENS * a.act.groups * GROUP;
-        s_from += TOKENS * a.act.groups;
-    }
-    __device__ __forceinline__ void store(char *buffer, int k) const
-    {
-        const int tid = threadIdx.x;
-        if (k < Z) {
-            const int t = tid / Z_WORDS + k * (GRAD_THREADS / Z_WORDS);
-            if constexpr (sizeof(T) == 2) {
-                *reinterpret_cast<u32x4 *>(buffer + t * GRAD_PITCH + tid % Z_WORDS * 16) = z[k];
-            } else {
-                ThreeParts p[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) p[i] = three_parts(__uint_as_float(z[k][i]));
-                char *at = buffer + t * GRAD_PITCH + tid % Z_WORDS * 8;
-                *reinterpret_cast<u32x2 *>(at) = u32x2{p[0].a >> 16 | p[1].a, p[2].a >> 16 | p[3].a};
-                *reinterpret_cast<u32x2 *>(at + TOKENS * GRAD_PITCH) = u32x2{p[0].b >> 16 | p[1].b, p[2].b >> 16 | p[3].b};
-                *reinterpret_cast<u32x2 *>(at + 2 * TOKENS * GRAD_PITCH) = u32x2{p[0].c >> 16 | p[1].c, p[2].c >> 16 | p[3].c};
-            }
-        } else {
-            k -= Z;
-            const int t = tid / 16 + k * (GRAD_THREADS / 16);
-            const float scale = scale_value(s[k]);
-            char *at = buffer + (PARTS * TOKENS + t) * GRAD_PITCH + tid % 16 * 32;
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const u32x2 lo = decode_four(x[k][2 * h], scale), hi = decode_four(x[k][2 * h + 1], scale);
-                *reinterpret_cast<u32x4 *>(at + 16 * h) = u32x4{lo.x, lo.y, hi.x, hi.y};
-            }
-        }
+        z_base += TOKENS * a.dz_stride * (int64_t)sizeof(T);
+        x_base += TOKENS * a.act.groups * GROUP;
+        s_base += TOKENS * a.act.groups;
     }
 
-    // The same for the step at token0, element by element and nothing read that is not there; zeros in its place.
-    static __device__ void fill(const GradArgs &a, int64_t token0, int64_t o0, int64_t n0, char *buffer)
+    // The step at token0 with zeros in the place of what is not there: whole words where a row has them, else element by element.  All loads are
+    // on their way before the first is used.
+    __device__ __forceinline__ void load_guarded(const GradArgs &a, int d, int64_t token0, int64_t o0, int64_t n0)
     {
-        for (int k = threadIdx.x; k < TOKENS * GRAD_TILE; k += GRAD_THREADS) {
-            const int t = k / GRAD_TILE, c = k % GRAD_TILE;
-            const bool there = token0 + t < a.rows;
-            char *at = buffer + t * GRAD_PITCH + c * 2;
-            unsigned v = 0;
-            if (there && o0 + c < a.out) v = element_bits(static_cast<const T *>(a.dz) + (token0 + t) * a.dz_stride + o0 + c);
+        const int64_t o = o0 + z_word() * Z_ELEMS, i = n0 + x_word() * 16, end = a.rows - 1;
+        const EF_GLOBAL T *dz = (const EF_GLOBAL T *)a.dz;
+        if (o + Z_ELEMS <= a.out) {
+#pragma unroll
+            for (int k = 0; k < Z; ++k) {
+                const EF_GLOBAL T *p = dz + min(token0 + z_row() + k * Z_ROWS, end) * a.dz_stride + o;
+                if constexpr (sizeof(T) == 2)
+                    z[d][k] = *(const EF_GLOBAL u32x4_any *)p;
+                else
+                    z[d][k] = *(const EF_GLOBAL u32x4_word *)p;
+            }
+        } else if (o < a.out) {
+#pragma unroll
+            for (int k = 0; k < Z; ++k) {
+                const EF_GLOBAL T *p = dz + min(token0 + z_row() + k * Z_ROWS, end) * a.dz_stride;
+                unsigned e[Z_ELEMS];
+#pragma unroll
+                for (int j = 0; j < Z_ELEMS; ++j) {
+                    if constexpr (sizeof(T) == 2)
+                        e[j] = *(const EF_GLOBAL uint16_t *)(p + min(o + j, a.out - 1));
+                    else
+                        e[j] = *(const EF_GLOBAL unsigned *)(p + min(o + j, a.out - 1));
+                }
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    if constexpr (sizeof(T) == 2)
+                        z[d][k][j] = e[2 * j] | e[2 * j + 1] << 16;
+                    else
+                        z[d][k][j] = e[j];
+                }
+            }
+        }
+        const bool there = i < a.act.groups * GROUP;
+        const EF_GLOBAL uint8_t *codes = (const EF_GLOBAL uint8_t *)a.act.codes, *scales = (const EF_GLOBAL uint8_t *)a.act.scales;
+#pragma unroll
+        for (int k = 0; k < X; ++k) {
+            const int64_t t = min(token0 + x_row() + k * X_ROWS, end);
+            x[d][k] = *(const EF_GLOBAL u32x4 *)(codes + t * a.act.groups * GROUP + (there ? i : 0));
+            s[d][k] = scales[t * a.act.groups + (there ? i / GROUP : 0)];
+        }
+#pragma unroll
+        for (int k = 0; k < Z; ++k)
+            if (o >= a.out || token0 + z_row() + k * Z_ROWS > end) z[d][k] = u32x4{0, 0, 0, 0};
+#pragma unroll
+        for (int k = 0; k < X; ++k)
+            if (!there || token0 + x_row() + k * X_ROWS > end) {
+                x[d][k] = u32x4{0, 0, 0, 0};
+                s[d][k] = SCALE_MIN;
+            }
+    }
+
+    // What is carried goes to LDS in pieces of about four instructions, as many as hide behind one product; where RELOAD is set, each word's last piece
+    // asks for the next step's.  A word of bf16: one piece.  A word of codes: four.  A word of fp32: its elements' second parts, the third ones two at
+    // a time, then a part of all four to LDS at a time.
+    static constexpr int Z_PIECES = sizeof(T) == 2 ? 1 : 9, X_PIECES = 4;
+    static constexpr int PIECES = Z * Z_PIECES + X * X_PIECES;
+    float rest[sizeof(T) == 2 ? 1 : 4];
+    unsigned third[sizeof(T) == 2 ? 1 : 4];
+    u32x2 held;
+    template <int Q, bool RELOAD>
+    __device__ __forceinline__ void piece(const GradArgs &a, int d, char *buffer)
+    {
+        if constexpr (Q < Z * Z_PIECES) {
+            constexpr int k = Q / Z_PIECES, part = Q % Z_PIECES;
+            char *at = buffer + (z_row() + k * Z_ROWS) * PITCH + z_word() * (2 * Z_ELEMS);
             if constexpr (sizeof(T) == 2) {
-                *reinterpret_cast<uint16_t *>(at) = (uint16_t)v;
+                *reinterpret_cast<u32x4 *>(at) = z[d][k];
+                if (RELOAD) load_z(a, d, k);
+            } else if constexpr (part < 4) {
+                rest[part] = cut_off(__uint_as_float(z[d][k][part]));
+            } else if constexpr (part < 6) {
+#pragma unroll
+                for (int e = 2 * (part - 4); e < 2 * (part - 4) + 2; ++e) third[e] = __float_as_uint(rest[e] - upper(rest[e]));
+            } else if constexpr (part == 6) {
+                *reinterpret_cast<u32x2 *>(at) = u32x2{uppers(z[d][k][0], z[d][k][1]), uppers(z[d][k][2], z[d][k][3])};
+                if (RELOAD) load_z(a, d, k);
+            } else if constexpr (part == 7) {
+                *reinterpret_cast<u32x2 *>(at + TOKENS * PITCH) =
+                    u32x2{uppers(__float_as_uint(rest[0]), __float_as_uint(rest[1])), uppers(__float_as_uint(rest[2]), __float_as_uint(rest[3]))};
             } else {
-                const ThreeParts p = three_parts(__uint_as_float(v));
-                *reinterpret_cast<uint16_t *>(at) = (uint16_t)(p.a >> 16);
-                *reinterpret_cast<uint16_t *>(at + TOKENS * GRAD_PITCH) = (uint16_t)(p.b >> 16);
-                *reinterpret_cast<uint16_t *>(at + 2 * TOKENS * GRAD_PITCH) = (uint16_t)(p.c >> 16);
+                *reinterpret_cast<u32x2 *>(at + 2 * TOKENS * PITCH) = u32x2{uppers(third[0], third[1]), uppers(third[2], third[3])};
             }
-            uint16_t x = 0;
-            if (there && n0 + c < a.n) {
-                const unsigned code = *a.act.code_at(token0 + t, n0 + c), scale = *a.act.scale_at(token0 + t, n0 + c);
-                x = (uint16_t)decode_four(code, scale_value(scale)).x;
+        } else {
+            constexpr int k = (Q - Z * Z_PIECES) / X_PIECES, part = (Q - Z * Z_PIECES) % X_PIECES, h = part / 2;
+            const float scale = scale_value(s[d][k]);
+            if constexpr (part % 2 == 0) {
+                held = decode_four(x[d][k][2 * h], scale);
+            } else {
+                const u32x2 more = decode_four(x[d][k][2 * h + 1], scale);
+                char *at = buffer + (PARTS * TOKENS + x_row() + k * X_ROWS) * PITCH + x_word() * 32;
+                *reinterpret_cast<u32x4 *>(at + 16 * h) = u32x4{held.x, held.y, more.x, more.y};
+                if constexpr (h == 1 && RELOAD) load_x(a, d, k);
             }
-            *reinterpret_cast<uint16_t *>(buffer + (PARTS * TOKENS + t) * GRAD_PITCH + c * 2) = x;
         }
     }
 };
 
-// Eight tokens of a channel to a lane: lane l gets channel l % 32 and tokens l / 32 * 8 + 0..7 of the 32 channels x 16 tokens at p (p: the
-// lane's own place, see grad_lane_offset).
-__device__ __forceinline__ bf16x8 read_transposed(const char *p)
-{
-    typedef __attribute__((address_space(3))) s16x4 shared_s16x4;
-    const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((shared_s16x4 *)(p));
-    const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((shared_s16x4 *)(p + 4 * GRAD_PITCH));
-    typedef short s16x8 __attribute__((ext_vector_type(8)));
-    return __builtin_bit_cast(bf16x8, (s16x8)__builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
-}
+template <class F, int... I>
+__device__ __forceinline__ void times(F f, std::integer_sequence<int, I...>) { (f(std::integral_constant<int, I>()), ...); }
+// f(0), f(1), ... f(N - 1), the index known to the compiler
+template <int N, class F>
+__device__ __forceinline__ void times(F f) { times(f, std::make_integer_sequence<int, N>()); }
+
+// Eight tokens of a channel to a lane, in two reads of four: lane l gets channel l % 32 and tokens l / 32 * 8 + 0..7 of the 32 channels x 16
+// tokens at p (p: the lane's own place, see grad_lane_offset).
+struct Fragment {
+    s16x4 half[2];
+    template <int PITCH>
+    __device__ __forceinline__ void read(const char *p, int h)
+    {
+        typedef __attribute__((address_space(3))) s16x4 shared_s16x4;
+        half[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((shared_s16x4 *)(p + h * 4 * PITCH));
+    }
+    __device__ __forceinline__ bf16x8 whole() const
+    {
+        return __builtin_bit_cast(bf16x8, (s16x8)__builtin_shufflevector(half[0], half[1], 0, 1, 2, 3, 4, 5, 6, 7));
+    }
+};
 // 16 lanes read four tokens x 16 channels, lane i of them four channels of token i / 4 (and get four tokens of channel i).
-__device__ __forceinline__ int grad_lane_offset(int lane)
+__device__ __forceinline__ int grad_lane_offset(int lane, int pitch)
 {
     const int block = lane / 16, i = lane % 16;
-    return ((block >> 1) * 8 + i / 4) * GRAD_PITCH + ((block & 1) * 16 + i % 4 * 4) * 2;
+    return ((block >> 1) * 8 + i / 4) * pitch + ((block & 1) * 16 + i % 4 * 4) * 2;
 }
 
-template <class T>
-__global__ __launch_bounds__(GRAD_THREADS, 1) void k_weight_grad(GradArgs a)
-{
-    constexpr int TOKENS = GradStep<T>::TOKENS, PARTS = GradStep<T>::PARTS;
-    __shared__ __align__(16) char buffers[2][GRAD_ROWS * GRAD_PITCH];
-    // Workgroups go to the eight XCDs in turn: each XCD takes a run of neighbouring tiles, which share rows of dz in its L2.
-    const int n_tiles = a.tiles_out * a.tiles_n, all = n_tiles * a.splits;
-    int id = blockIdx.x;
+// What follows product m of region r of a 256 x 256 tile's step (sixteen products on one set of fragments): the pieces from piece[16 r + m] on up to the
+// next entry, and the halves reads[m] .. reads[m + 1] of the next region's fragments, all on their way twelve products after the region's first.
+template <int REGIONS, int PIECES>
+struct GradSchedule {
+    int piece[(REGIONS - 1) * 16 + 17] = {}, reads[17] = {};
+    constexpr GradSchedule()
     {
-        const int per = all / 8, more = all % 8, xcd = id % 8, k = id / 8;
-        id = xcd * per + min(xcd, more) + k;
+        constexpr int SLOTS = (REGIONS - 1) * 16;
+        for (int k = 0; k < SLOTS + 17; ++k) piece[k] = k < SLOTS ? k * PIECES / SLOTS : PIECES;
+        int sum = 0;
+        for (int m = 0; m < 17; ++m) {
+            reads[m] = sum < 16 ? sum : 16;
+            sum += m % 4 == 0 ? 2 : 1;
+        }
     }
-    const int split = id / n_tiles, tile = id % n_tiles;
-    const int64_t o0 = (int64_t)(tile / a.tiles_n) * GRAD_TILE, n0 = (int64_t)(tile % a.tiles_n) * GRAD_TILE;
-    const int64_t first = a.steps * split / a.splits, last = a.steps * (split + 1) / a.splits;
+};
+
+// A step is REGIONS sets of SIDE x SIDE products a wavefront.  With SIDE = 4 there is one wavefront to a SIMD: what it does besides products has to
+// hide behind them, about four instructions of 4 to 6 cycles to a product's 32 (measured: one more costs its own time).  So everything is
+// given its place (GradSchedule): fragments are read a region ahead, words of the next step go to LDS piece by piece, and the words of the one behind
+// it are asked for as the registers get free; one barrier a step.  Smaller tiles have several workgroups on a CU that hide one another's waits.
+template <class T, int SIDE>
+__global__ __launch_bounds__(GRAD_THREADS, SIDE == 4 ? 1 : 2) void k_weight_grad(GradArgs a)
+{
+    using Stage = GradStage<T, SIDE>;
+    constexpr int TOKENS = Stage::TOKENS, PARTS = Stage::PARTS, TILE = Stage::TILE, PITCH = Stage::PITCH, REGIONS = TOKENS / 16 * PARTS;
+    __shared__ __align__(16) char buffers[2][GRAD_ROWS * PITCH];
+    // Workgroups go to the eight XCDs in turn: each XCD takes a run of neighbouring tiles, which share rows of dz in its L2.
+    const auto in_runs = [](int id, int all) { return id % 8 * (all / 8) + min(id % 8, all % 8) + id / 8; };
+    int tile, split = 0, splits = 1;
+    if ((int)blockIdx.x < a.whole) {
+        tile = in_runs(blockIdx.x, a.whole);
+    } else {
+        const int cut = a.tiles - a.whole, id = in_runs(blockIdx.x - a.whole, cut * a.splits);
+        splits = a.splits;
+        split = id / cut;
+        tile = a.whole + id % cut;
+    }
+    const int64_t o0 = (int64_t)(tile / a.tiles_n) * TILE, n0 = (int64_t)(tile % a.tiles_n) * TILE;
+    const int64_t first = a.steps * split / splits, last = a.steps * (split + 1) / splits, safe = min(last, Stage::unsafe(a, o0));
 
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-    const int z_at = grad_lane_offset(lane) + wave / 2 * 256;
-    const int x_at = grad_lane_offset(lane) + wave % 2 * 256 + PARTS * TOKENS * GRAD_PITCH;
-    f32x16 acc[4][4];
+    const int z_at = grad_lane_offset(lane, PITCH) + wave / 2 * TILE;
+    const int x_at = grad_lane_offset(lane, PITCH) + wave % 2 * TILE + PARTS * TOKENS * PITCH;
+    f32x16 acc[SIDE][SIDE];
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < SIDE; ++i)
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
+        for (int j = 0; j < SIDE; ++j)
 #pragma unroll
             for (int k = 0; k < 16; ++k) acc[i][j][k] = 0.0f;
 
-    // Steps before `safe` read nothing past dz's end: a token's last word may reach seven elements past its row.
-    const int64_t spare = o0 + GRAD_TILE <= a.out ? 0 : (7 + a.dz_stride - 1) / a.dz_stride;
-    const int64_t safe = min(last, (a.rows - spare) / TOKENS);
-    constexpr int REGIONS = TOKENS / 16 * PARTS, WORDS = GradStage<T>::Z + GradStage<T>::X;
-    bf16x8 z[2][4], x[2][4];
-    // fragment f of region r: x's where a region begins with another sixteen tokens, then dz's
-    auto fragment = [&](const char *buffer, int r, int f) {
-        const int k = r / PARTS, p = r % PARTS;
-        if (f < 4) {
-            if (p == 0) x[k & 1][f] = read_transposed(buffer + x_at + k * 16 * GRAD_PITCH + f * 64);
+    Fragment z[2][SIDE], x[2][SIDE];
+    // Half h of region r's fragments, x's first; those only where a region begins with another sixteen tokens.
+    auto fragment = [&](const char *buffer, int r, int h) {
+        const int k = r / PARTS, p = r % PARTS, f = h / 2;
+        if (f < SIDE) {
+            if (p == 0) x[k & 1][f].template read<PITCH>(buffer + x_at + k * 16 * PITCH + f * 64, h % 2);
         } else {
-            z[r & 1][f - 4] = read_transposed(buffer + z_at + (p * TOKENS + k * 16) * GRAD_PITCH + (f - 4) * 64);
+            z[r & 1][f - SIDE].template read<PITCH>(buffer + z_at + (p * TOKENS + k * 16) * PITCH + (f - SIDE) * 64, h % 2);
         }
     };
     auto product = [&](int r, int i, int j) {
-        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(z[r & 1][i], x[r / PARTS & 1][j], acc[i][j], 0, 0, 0);
+        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(z[r & 1][i].whole(), x[r / PARTS & 1][j].whole(), acc[i][j], 0, 0, 0);
     };
-    int64_t step = first;
     char *now = buffers[0], *next = buffers[1];
-    GradStage<T> stage;
-    stage.begin(a, first * TOKENS, o0, n0);
-    if (first < safe) {
-#pragma unroll
-        for (int k = 0; k < WORDS; ++k) stage.load(a, k);
-        if (first + 1 < safe) stage.next(a);
-#pragma unroll
-        for (int k = 0; k < WORDS; ++k) {
-            stage.store(now, k);
-            stage.load(a, k);
-        }
-        if (first + 2 < safe) stage.next(a);
-    } else if (first < last) {
-        GradStage<T>::fill(a, first * TOKENS, o0, n0, now);
-    }
-    __syncthreads();
-    if (step + 1 < safe) {
-#pragma unroll
-        for (int f = 0; f < 8; ++f) fragment(now, 0, f);
-        for (; step + 1 < safe; ++step) {
-#pragma unroll
-            for (int r = 0; r < REGIONS; ++r) {
-                if (r == REGIONS - 1) __syncthreads();
-#pragma unroll
-                for (int m = 0; m < 16; ++m) {
-                    product(r, m / 4, m % 4);
-                    if (m < 8) {
-                        if (r < REGIONS - 1)
-                            fragment(now, r + 1, m);
-                        else
-                            fragment(next, 0, m);
-                    } else if (r < REGIONS - 1) {
-                        // words of the next step to LDS, those of the one behind it on their way into the same registers
-                        constexpr int EACH = (WORDS + REGIONS - 2) / (REGIONS - 1);
-                        const int w = r * EACH + (m - 8) / 2;
-                        if (m % 2 == 0 && (m - 8) / 2 < EACH && w < WORDS) {
-                            stage.store(next, w);
-                            stage.load(a, w);
-                        }
-                    }
-                    __builtin_amdgcn_sched_barrier(0);
-                }
-            }
-            if (step + 3 < safe) stage.next(a);
-            char *t = now;
-            now = next;
-            next = t;
-        }
-    }
-    for (; step < last; ++step) {
-        if (step + 1 < last) GradStage<T>::fill(a, (step + 1) * TOKENS, o0, n0, next);
-#pragma unroll
-        for (int r = 0; r < REGIONS; ++r) {
-#pragma unroll
-            for (int f = 0; f < 8; ++f) fragment(now, r, f);
-#pragma unroll
-            for (int m = 0; m < 16; ++m) product(r, m / 4, m % 4);
-        }
-        __syncthreads();
+    auto turn = [&] {
         char *t = now;
         now = next;
         next = t;
+    };
+    Stage stage;
+    int64_t step = first;
+    stage.begin(a, first * TOKENS, o0, n0);
+    auto fetch = [&](int64_t q, int d) {
+        if (q < safe) {
+            stage.load(a, d);
+            stage.next(a);
+        } else if (q < last) {
+            stage.load_guarded(a, d, q * TOKENS, o0, n0);
+        }
+    };
+    auto put = [&](int d, char *buffer) { times<Stage::PIECES>([&](auto q) { stage.template piece<q.value, false>(a, d, buffer); }); };
+    if (first < last) {
+#pragma unroll
+        for (int d = 0; d < Stage::DEPTH; ++d) fetch(first + d, d);
+        put(0, now);
+        if constexpr (SIDE == 4) {
+            if (first + 1 < safe) {
+                stage.load(a, 0);
+                if (first + 2 < safe) stage.next(a);
+            }
+        }
+    }
+    __syncthreads();
+    if constexpr (SIDE == 4) {
+        if (step + 1 < safe) {
+#pragma unroll
+            for (int h = 0; h < 16; ++h) fragment(now, 0, h);
+            // Behind the products of all regions but a step's last, pieces of the next step go to LDS and the next region's fragments are read.  The last
+            // region begins with the barrier and reads the next step's first fragments.
+            for (; step + 1 < safe; ++step) {
+                times<REGIONS * 16>([&](auto slot) {
+                    constexpr int r = slot.value / 16, m = slot.value % 16;
+                    constexpr GradSchedule<REGIONS, Stage::PIECES> PLAN;
+                    if constexpr (slot.value == REGIONS * 16 - 16) __syncthreads();
+                    product(r, m / 4, m % 4);
+                    times<PLAN.reads[m + 1] - PLAN.reads[m]>(
+                        [&](auto h) { fragment(r < REGIONS - 1 ? now : next, (r + 1) % REGIONS, PLAN.reads[m] + h.value); });
+                    times<PLAN.piece[slot.value + 1] - PLAN.piece[slot.value]>(
+                        [&](auto q) { stage.template piece<PLAN.piece[slot.value] + q.value, true>(a, 0, next); });
+                    __builtin_amdgcn_sched_barrier(0);
+                });
+                if (step + 3 < safe) stage.next(a);     // else the same words again, which nobody uses
+                turn();
+            }
+        }
+    }
+    auto products = [&] {
+#pragma unroll
+        for (int r = 0; r < REGIONS; ++r) {
+#pragma unroll
+            for (int h = 0; h < 4 * SIDE; ++h) fragment(now, r, h);
+#pragma unroll
+            for (int m = 0; m < SIDE * SIDE; ++m) product(r, m / SIDE, m % SIDE);
+        }
+    };
+    if constexpr (SIDE < 4) {
+        // without a branch: behind one, a wait for a load would be a wait for all behind it too
+        for (; step + 2 * Stage::DEPTH <= safe; step += Stage::DEPTH) {
+            times<Stage::DEPTH>([&](auto d) {
+                stage.load(a, d.value);
+                stage.next(a);
+                products();
+                put((d.value + 1) % Stage::DEPTH, next);
+                __syncthreads();
+                turn();
+            });
+        }
+    }
+    for (; step < last; step += Stage::DEPTH) {
+        times<Stage::DEPTH>([&](auto d) {
+            if (step + d.value >= last) return;
+            fetch(step + d.value + Stage::DEPTH, d.value);
+            products();
+            if (step + d.value + 1 < last) put((d.value + 1) % Stage::DEPTH, next);
+            __syncthreads();
+            turn();
+        });
     }
 
     // An accumulator's lane holds channel lane % 32 of x's side and four runs of four of dz's.
-    float *const dw = a.dw + (a.splits > 1 ? (int64_t)split * a.out * a.n : 0) + (o0 + wave / 2 * 128 + 4 * (lane / 32)) * a.n;
-    const bool whole = a.splits == 1;
-    const int64_t left = a.out - (o0 + wave / 2 * 128 + 4 * (lane / 32));
+    const int r0 = wave / 2 * (TILE / 2) + 4 * (lane / 32), c0 = wave % 2 * (TILE / 2) + lane % 32;
+    if ((int)blockIdx.x >= a.whole) {
+        float *const at = a.parts + ((int64_t)(tile - a.whole) * splits + split) * (TILE * TILE) + r0 * TILE + c0;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const int64_t i = n0 + wave % 2 * 128 + j * 32 + lane % 32;
-        if (i >= a.n) continue;
-        const float s = whole && a.scale ? a.scale[i] : 1.0f;
+        for (int i = 0; i < SIDE; ++i)
 #pragma unroll
-        for (int m = 0; m < 4; ++m) {
+            for (int j = 0; j < SIDE; ++j)
+#pragma unroll
+                for (int k = 0; k < 16; ++k) at[(i * 32 + 8 * (k / 4) + k % 4) * TILE + j * 32] = acc[i][j][k];
+        return;
+    }
+    float *const dw = a.dw + (o0 + r0) * a.n;
+    const int64_t left = a.out - (o0 + r0);
+#pragma unroll
+    for (int j = 0; j < SIDE; ++j) {
+        const int64_t c = n0 + c0 + j * 32;
+        if (c >= a.n) continue;
+        const float s = a.scale ? a.scale[c] : 1.0f;
+#pragma unroll
+        for (int i = 0; i < SIDE; ++i) {
             float v[16];
 #pragma unroll
-            for (int k = 0; k < 16; ++k) v[k] = acc[m][j][k] * s;
-            float *const at = dw + m * 32 * a.n + i;
-            if (whole && a.accumulate) {
+            for (int k = 0; k < 16; ++k) v[k] = acc[i][j][k] * s;
+            float *const at = dw + i * 32 * a.n + c;
+            if (a.accumulate) {
                 float old[16];
 #pragma unroll
-                for (int k = 0; k < 16; ++k) old[k] = m * 32 + 8 * (k / 4) + k % 4 < left ? at[(8 * (k / 4) + k % 4) * a.n] : 0.0f;
+                for (int k = 0; k < 16; ++k) old[k] = i * 32 + 8 * (k / 4) + k % 4 < left ? at[(8 * (k / 4) + k % 4) * a.n] : 0.0f;
 #pragma unroll
                 for (int k = 0; k < 16; ++k) v[k] += old[k];
             }
 #pragma unroll
             for (int k = 0; k < 16; ++k)
-                if (m * 32 + 8 * (k / 4) + k % 4 < left) at[(8 * (k / 4) + k % 4) * a.n] = v[k];
+                if (i * 32 + 8 * (k / 4) + k % 4 < left) at[(8 * (k / 4) + k % 4) * a.n] = v[k];
         }
     }
 }
 
-// dw <- [dw +] scale * the sum of the splits' results, in their order.
-__global__ __launch_bounds__(256) void k_join_splits(const float *parts, int splits, int64_t out, int64_t n, const float *scale, float *dw,
-                                                     int accumulate)
+// dw <- [dw +] scale * the sum of the splits' results, in their order: four neighbouring channels to a thread.
+template <int TILE>
+__global__ __launch_bounds__(256) void k_join_splits(GradArgs a)
 {
-    const int64_t total = out * n;
-    for (int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x; at < total; at += (int64_t)gridDim.x * 256) {
-        float s = parts[at];
-        for (int p = 1; p < splits; ++p) s += parts[(int64_t)p * total + at];
-        if (scale) s *= scale[at % n];
-        dw[at] = accumulate ? dw[at] + s : s;
+    constexpr int EACH = TILE * TILE / 4 / 256;         // workgroups to a tile
+    const int cut = blockIdx.x / EACH, tile = a.whole + cut, at = (blockIdx.x % EACH * 256 + threadIdx.x) * 4;
+    const int64_t o = (int64_t)(tile / a.tiles_n) * TILE + at / TILE, i = (int64_t)(tile % a.tiles_n) * TILE + at % TILE;
+    if (o >= a.out || i >= a.n) return;
+    const float *from = a.parts + (int64_t)cut * a.splits * (TILE * TILE) + at;
+    float v[4] = {};
+    for (int p = 0; p < a.splits; p += 8) {
+        u32x4 w[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            if (p + k < a.splits) w[k] = *reinterpret_cast<const u32x4 *>(from + (int64_t)(p + k) * (TILE * TILE));
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            if (p + k < a.splits) {
+#pragma unroll
+                for (int c = 0; c < 4; ++c) v[c] += __uint_as_float(w[k][c]);
+            }
     }
+    float *dw = a.dw + o * a.n + i;
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+        if (i + c < a.n) {
+            const float s = a.scale ? v[c] * a.scale[i + c] : v[c];
+            dw[c] = a.accumulate ? dw[c] + s : s;
+        }
 }
 
 }  // namespace ef

@@ -161,23 +161,55 @@ int policy_args(int64_t rows, int64_t vocab, int type, const void *logits, int64
     return EF_OK;
 }
 
-// How many parts the tokens are cut into: a weight gradient of few tiles leaves CUs without work, a part more costs
-// the writing and reading of a partial result.
-int grad_splits(int64_t tiles, int64_t steps, int64_t out, int64_t n)
+// How a weight gradient is cut: the tile's side, and for the tiles that do not fill a round of the CUs the number of parts along the tokens.
+struct GradCut {
+    int side;
+    int64_t tiles_n, tiles, whole;
+    int splits;
+};
+
+// The choice is the least of a sum of what was measured: a step of a tile of 256, 128 or 64 channels takes `alone` us with few workgroups on the GPU and
+// `loaded` us with as many as it holds (`most` on a CU; more slow the others down with the square of their share), a launch and a workgroup's
+// beginning and end `base`, and joining parts 4 us and 0.3 for each MB of them.  Large tiles win where there are many (4096 x 4096, 4096
+// tokens, bf16: 113, 171 and 286 us), small ones where there are few tokens (1024 x 1024, 1024 tokens: 33, 16 and 9 us), parts where there are
+// many (200 x 200, 8000 tokens, tiles of 64: 42 us in one part, 12 in 8 to 16).
+GradCut grad_cut(int type, int64_t steps, int64_t out, int64_t n)
 {
-    int best = 1;
+    struct Side { int side, most; double alone, loaded, base; };
+    static constexpr Side SIDES[2][3] = {{{4, 1, 1.7, 2.3, 15.0}, {2, 2, 0.75, 1.55, 6.0}, {1, 3, 0.44, 0.82, 5.5}},         // EF_TYPE_FP32
+                                         {{4, 1, 1.14, 1.5, 15.0}, {2, 2, 0.64, 1.25, 6.0}, {1, 2, 0.3, 0.55, 5.5}}};
+    GradCut best{};
     double least = 0.0;
-    for (int64_t k = 1; k <= 64 && k <= std::max<int64_t>(1, steps / 2); ++k) {
-        if (k > 1 && k * out * n > PART_FLOATS) break;
-        const double rounds = (double)ceil_div(tiles * k, 256) * ((double)ceil_div(steps, k) + 3.0);       // in steps of about 1 us
-        const double join = k > 1 ? 4.0 + (double)(k + 1) * (double)out * (double)n * 4.0 / 4.0e6 : 0.0;
-        const double cost = rounds + join;
-        if (k == 1 || cost < least) {
-            best = (int)k;
-            least = cost;
+    for (const Side &c : SIDES[type == EF_TYPE_BF16]) {
+        const int64_t tile = 64 * c.side, tiles_n = ceil_div(n, tile), tiles = ceil_div(out, tile) * tiles_n, round = 256 * c.most;
+        const int64_t whole = tiles / round * round, cut = tiles - whole;
+        const auto took = [&](int64_t groups, int64_t of) {
+            const double share = (double)std::min(groups, round) / (double)round;
+            return (double)(ceil_div(groups, round) * of) * (c.alone + (c.loaded - c.alone) * share * share);
+        };
+        for (int64_t splits = 1; splits <= 64 && splits <= std::max<int64_t>(1, steps); ++splits) {
+            const int64_t part = cut * splits * tile * tile;
+            if (splits > 1 && (cut == 0 || part > PART_FLOATS)) break;
+            const double cost = c.base + took(whole, steps) + took(cut * splits, ceil_div(steps, splits)) +
+                                (splits > 1 ? 4.0 + 0.3 * (double)part * 4.0 / 1e6 : 0.0);
+            if (best.side == 0 || cost < least) {
+                best = GradCut{c.side, tiles_n, tiles, splits > 1 ? whole : tiles, (int)splits};
+                least = cost;
+            }
         }
     }
     return best;
+}
+
+template <class T, int SIDE>
+void launch_weight_grad(const ef::GradArgs &a, hipStream_t s)
+{
+    const int64_t cut = a.tiles - a.whole;
+    hipLaunchKernelGGL((ef::k_weight_grad<T, SIDE>), dim3((unsigned)(a.whole + cut * a.splits)), dim3(ef::GRAD_THREADS), 0, s, a);
+    if (cut) {
+        constexpr int TILE = 64 * SIDE;
+        hipLaunchKernelGGL(ef::k_join_splits<TILE>, dim3((unsigned)(cut * (TILE * TILE / 1024))), dim3(256), 0, s, a);
+    }
 }
 
 }  // namespace
@@ -344,22 +376,22 @@ int ef_weight_grad(ef_workspace *workspace, int64_t rows, int64_t out_width, int
     a.act = act_ref(act, rows, width);
     a.scale = column_scale;
     a.accumulate = accumulate ? 1 : 0;
-    const int64_t tiles_out = ceil_div(out_width, ef::GRAD_TILE), tiles_n = ceil_div(width, ef::GRAD_TILE);
     a.steps = ceil_div(rows, type == EF_TYPE_BF16 ? ef::GradStep<ef::bf16_t>::TOKENS : ef::GradStep<float>::TOKENS);
-    if (tiles_out * tiles_n > 0x1ffffff) return EF_ERR_SIZE;
-    a.tiles_out = (int)tiles_out;
-    a.tiles_n = (int)tiles_n;
-    a.splits = grad_splits(tiles_out * tiles_n, a.steps, out_width, width);
-    a.dw = a.splits > 1 ? workspace->parts : dw;
-    const dim3 grid((unsigned)(tiles_out * tiles_n * a.splits));
-    EF_BY_TYPE(type, T, hipLaunchKernelGGL(ef::k_weight_grad<T>, grid, dim3(ef::GRAD_THREADS), 0, s, a));
+    const GradCut c = grad_cut(type, a.steps, out_width, width);
+    if (c.tiles > 0x1ffffff) return EF_ERR_SIZE;
+    a.dw = dw;
+    a.parts = workspace->parts;
+    a.tiles = (int)c.tiles;
+    a.tiles_n = (int)c.tiles_n;
+    a.whole = (int)c.whole;
+    a.splits = c.splits;
+    if (c.side == 4)
+        EF_BY_TYPE(type, T, launch_weight_grad<T, 4>(a, s));
+    else if (c.side == 2)
+        EF_BY_TYPE(type, T, launch_weight_grad<T, 2>(a, s));
+    else
+        EF_BY_TYPE(type, T, launch_weight_grad<T, 1>(a, s));
     EF_HIP(hipGetLastError());
-    if (a.splits > 1) {
-        const int64_t groups = std::min(ceil_div(out_width * width, 256), (int64_t)4096);
-        hipLaunchKernelGGL(ef::k_join_splits, dim3((unsigned)groups), dim3(256), 0, s, workspace->parts, a.splits, out_width, width,
-                           column_scale, dw, a.accumulate);
-        EF_HIP(hipGetLastError());
-    }
     return EF_OK;
 }
 

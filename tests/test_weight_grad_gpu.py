@@ -12,6 +12,8 @@ pytestmark = pytest.mark.gpu
 # tokens, out, width: a token and a channel; ends inside a tile, a step, a group; several tiles; many steps, cut into splits
 SHAPES = [(1, 1, 1), (1, 257, 33), (15, 16, 40), (64, 256, 256), (65, 255, 257), (63, 31, 7), (129, 300, 1031), (2000, 24, 31),
           (5000, 130, 259), (700, 515, 1031), (4097, 513, 64)]
+# the same for the largest tile: few steps and many, one part and several, whole rounds and a rest
+LARGE = [(200, 8001, 2001), (65, 8001, 2001), (1100, 4133, 2071), (700, 16500, 1031), (3000, 3001, 1031)]
 
 
 def whole_numbers(rows, out, width, dtype, seed):
@@ -30,7 +32,7 @@ def encoded(x):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("rows,out,width", SHAPES)
+@pytest.mark.parametrize("rows,out,width", SHAPES + LARGE)
 def test_whole_numbers_exactly(rows, out, width, dtype):
     dz, x = whole_numbers(rows, out, width, dtype, rows + out)
     ws = ef.ef_workspace_create(rows)
