@@ -93,12 +93,6 @@ struct GradStage {
         const int64_t spare = o0 + TILE <= a.out ? 0 : (Z_ELEMS - 1 + a.dz_stride - 1) / a.dz_stride;
         return max((int64_t)0, a.rows - spare) / TOKENS;
     }
-    // An offset that is 32 bits wide where it is used: the load then adds it to a scalar base itself.
-    static __device__ __forceinline__ unsigned here(unsigned off)
-    {
-        asm volatile("" : "+v"(off));
-        return off;
-    }
     __device__ __forceinline__ void load_z(const GradArgs &a, int d, int k)
     {
         const EF_GLOBAL char *p = z_base + (int64_t)k * Z_ROWS * a.dz_stride * (int64_t)sizeof(T) + here(z_off);

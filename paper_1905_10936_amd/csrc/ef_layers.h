@@ -129,13 +129,16 @@ int launch_norm_backward(ef::NormBackward &a, hipStream_t s)
 template <class T, int LANES, int CHUNKS>
 void launch_policy(const ef::PolicyArgs &a, hipStream_t s)
 {
+    // as many workgroups as the CUs hold at most (2048 threads a CU); they go on to further rows
     constexpr int threads = ef::policy_threads(LANES);
-    hipLaunchKernelGGL((ef::k_policy<T, LANES, CHUNKS>), dim3((unsigned)ceil_div(a.rows, threads / LANES)), dim3(threads), 0, s, a);
+    const int64_t groups = std::min(ceil_div(a.rows, threads / LANES), (int64_t)256 * 2048 / threads);
+    hipLaunchKernelGGL((ef::k_policy<T, LANES, CHUNKS>), dim3((unsigned)groups), dim3(threads), 0, s, a);
 }
 
 template <class T>
 void policy_rows(const ef::PolicyArgs &a, hipStream_t s)
 {
+    // a wavefront up to 2048 entries (no barrier), 256 threads up to 8192, 1024 beyond, with as many eights a thread as the row takes
     const int64_t n = a.vocab;
     if (n <= 512)
         launch_policy<T, 64, 1>(a, s);
@@ -143,12 +146,18 @@ void policy_rows(const ef::PolicyArgs &a, hipStream_t s)
         launch_policy<T, 64, 4>(a, s);
     else if (n <= 8192)
         launch_policy<T, 256, 4>(a, s);
-    else if (n <= 32768)
-        launch_policy<T, 1024, 4>(a, s);
-    else if (n <= 65536)
-        launch_policy<T, 1024, 8>(a, s);
-    else
+    else if (n > 65536)
         hipLaunchKernelGGL(ef::k_policy_long<T>, dim3((unsigned)a.rows), dim3(ef::LONG_THREADS), 0, s, a);
+    else
+        switch ((n + 8191) / 8192) {
+        case 2: launch_policy<T, 1024, 2>(a, s); break;
+        case 3: launch_policy<T, 1024, 3>(a, s); break;
+        case 4: launch_policy<T, 1024, 4>(a, s); break;
+        case 5: launch_policy<T, 1024, 5>(a, s); break;
+        case 6: launch_policy<T, 1024, 6>(a, s); break;
+        case 7: launch_policy<T, 1024, 7>(a, s); break;
+        default: launch_policy<T, 1024, 8>(a, s); break;
+        }
 }
 
 int policy_args(int64_t rows, int64_t vocab, int type, const void *logits, int64_t stride, const int64_t *tokens)

@@ -28,20 +28,47 @@ struct PolicyArgs {
 constexpr float LOG2E = 1.44269502162933349609375f;     // log2(e) rounded to fp32
 constexpr float LN2 = 0.693147182464599609375f;
 
+// What a row's loss needs besides its logits, asked for a row ahead.
+struct RowArgs {
+    int64_t token;
+    float q, old, ref, adv;     // q: the row's weight, 0 if it is masked
+    __device__ __forceinline__ void load(const PolicyArgs &a, int64_t row)
+    {
+        token = a.tokens[row];
+        q = a.token_weight ? a.token_weight[row] : 1.0f;
+        old = a.logp_old ? a.logp_old[row] : 0.0f;
+        ref = a.logp_ref ? a.logp_ref[row] : 0.0f;
+        adv = a.loss ? a.advantage[row] : 0.0f;
+    }
+    // the same in scalar registers, where the wavefront has one row
+    __device__ __forceinline__ RowArgs scalar() const
+    {
+        const auto one = [](float v) { return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(v))); };
+        RowArgs s;
+        s.token = (int64_t)((uint64_t)(unsigned)__builtin_amdgcn_readfirstlane((unsigned)token) |
+                            (uint64_t)(unsigned)__builtin_amdgcn_readfirstlane((unsigned)((uint64_t)token >> 32)) << 32);
+        s.q = one(q);
+        s.old = one(old);
+        s.ref = one(ref);
+        s.adv = one(adv);
+        return s;
+    }
+    __device__ __forceinline__ bool masked(const PolicyArgs &a) const { return q == 0.0f || (uint64_t)token >= (uint64_t)a.vocab; }
+};
+
 // Loss of a row and its derivative with respect to logp, times the row's weight.
-__device__ __forceinline__ float2 row_loss(const PolicyArgs &a, int64_t row, float q, float logp)
+__device__ __forceinline__ float2 row_loss(const PolicyArgs &a, const RowArgs &w, float logp)
 {
-    const float adv = a.advantage[row];
-    const float r = a.logp_old ? expf(logp - a.logp_old[row]) : 1.0f;
-    const float free = r * adv, held = fminf(fmaxf(r, a.low), a.high) * adv;
+    const float r = a.logp_old ? expf(logp - w.old) : 1.0f;
+    const float free = r * w.adv, held = fminf(fmaxf(r, a.low), a.high) * w.adv;
     float f = -(free <= held ? free : held), c = free <= held ? -free : 0.0f;
     if (!(free == free) || !(held == held)) f = c = free + held;      // NaN
     if (a.logp_ref) {
-        const float d = a.logp_ref[row] - logp, m = expm1f(d);
+        const float d = w.ref - logp, m = expm1f(d);
         f += a.kl * (m - d);
         c -= a.kl * m;
     }
-    return make_float2(q * f, q * c);
+    return make_float2(w.q * f, w.q * c);
 }
 
 struct Exponent {
@@ -58,85 +85,137 @@ struct Exponent {
     __device__ __forceinline__ float log_sum(float sum, float top) const { return logf(sum) - LN2 * __builtin_fmaf(top, factor, -c); }
 };
 
-// What a row's token says about it: its weight, 0 for a masked row.
-__device__ __forceinline__ float row_weight(const PolicyArgs &a, int64_t row, int64_t token)
-{
-    if ((uint64_t)token >= (uint64_t)a.vocab) return 0.0f;
-    return a.token_weight ? a.token_weight[row] : 1.0f;
-}
-
 constexpr int policy_threads(int lanes) { return lanes < 256 ? 256 : lanes; }
 
+// A masked row's outputs.
+template <class T, int LANES>
+__device__ __forceinline__ void masked_row(const PolicyArgs &a, int64_t row, int lane)
+{
+    if (lane == 0) {
+        if (a.logp) a.logp[row] = 0.0f;
+        if (a.losses) a.losses[row] = 0.0f;
+    }
+    if (!a.dlogits) return;
+    T *g = static_cast<T *>(a.dlogits) + row * a.dlogits_stride;
+    Eight<T> zero;
+    zero.fill(0u);
+    for (int64_t i = (int64_t)lane * 8; i < a.vocab; i += LANES * 8) store_some(zero, g + i, a.vocab - i);
+}
+
+// A row as accesses see it: `head` elements up to the first 16-byte boundary, `whole` (a multiple of 8) from there, and the rest.  Accesses at
+// any place are allowed but slower: 4096 rows of 50257 in bf16, which start at odd places, take 210 us that way, 173 on boundaries.
+struct RowParts {
+    int head, whole;
+    template <class T>
+    __device__ __forceinline__ RowParts(const T *l, int vocab)
+    {
+        head = min(vocab, (int)(-(unsigned)(uintptr_t)l % 16u / sizeof(T)));
+        whole = (vocab - head) & ~7;
+    }
+    // of head and rest the one element that lane 0..15 takes: below 8 the head's, above the rest's; vocab or more: none
+    __device__ __forceinline__ int edge(int lane, int vocab) const
+    {
+        if (lane < 8) return lane < head ? lane : vocab;
+        return lane < 16 ? head + whole + lane - 8 : vocab;
+    }
+};
+
+// A team takes rows team, team + teams, ...; of a row, thread `lane` holds elements (c LANES + lane) 8 .. + 7 of its whole part for c < CHUNKS, and one
+// of its edges.
 template <class T, int LANES, int CHUNKS>
-__global__ __launch_bounds__(policy_threads(LANES)) void k_policy(PolicyArgs a)
+__global__ __launch_bounds__(policy_threads(LANES), LANES == 1024 && sizeof(T) * CHUNKS <= 16 ? 8 : 4) void k_policy(PolicyArgs a)
 {
     constexpr int TEAMS = policy_threads(LANES) / LANES;
     constexpr unsigned NONE = sizeof(T) == 2 ? 0xff80ff80u : 0xff800000u;       // -inf
-    __shared__ float tops[LANES > 64 ? LANES / 64 : 1], sums[LANES > 64 ? LANES / 64 : 1];
-    const int lane = threadIdx.x % LANES;
-    const int64_t row = (int64_t)blockIdx.x * TEAMS + threadIdx.x / LANES;
-    if (row >= a.rows) return;
-    const T *l = static_cast<const T *>(a.logits) + row * a.stride;
-    T *g = a.dlogits ? static_cast<T *>(a.dlogits) + row * a.dlogits_stride : nullptr;
-    const int64_t token = a.tokens[row];
-    const float q = row_weight(a, row, token);
-    if (q == 0.0f) {
-        if (lane == 0) {
-            if (a.logp) a.logp[row] = 0.0f;
-            if (a.losses) a.losses[row] = 0.0f;
+    __shared__ float tops[LANES > 64 ? LANES / 64 : 1], sums[LANES > 64 ? LANES / 64 : 1], slope;
+    const int lane = threadIdx.x % LANES, vocab = (int)a.vocab;
+    const unsigned off = lane * 8 * (unsigned)sizeof(T);
+    const int64_t teams = (int64_t)gridDim.x * TEAMS;
+    int64_t row = (int64_t)blockIdx.x * TEAMS + (TEAMS > 1 ? (int)__builtin_amdgcn_readfirstlane(threadIdx.x / LANES) : 0);
+    RowArgs next;
+    if (row < a.rows) next.load(a, row);
+    for (; row < a.rows; row += teams) {
+        const RowArgs w = next.scalar();
+        if (row + teams < a.rows) next.load(a, row + teams);
+        if (w.masked(a)) {
+            masked_row<T, LANES>(a, row, lane);
+            continue;
         }
-        if (g) {
-            Eight<T> zero;
-            zero.fill(0u);
-            for (int64_t i = (int64_t)lane * 8; i < a.vocab; i += LANES * 8) store_some(zero, g + i, a.vocab - i);
+        const T *l = static_cast<const T *>(a.logits) + row * a.stride;
+        const RowParts part(l, vocab);
+        const int whole = part.whole, last = part.edge(lane, vocab), chunks = (whole + LANES * 8 - 1) / (LANES * 8);
+        Eight<T> e[CHUNKS];
+#pragma unroll
+        for (int c = 0; c < CHUNKS; ++c) {
+            const int i = (c * LANES + lane) * 8;
+            e[c].fill(NONE);
+            if (i < whole) e[c].load_at(l + part.head + c * LANES * 8, off);
         }
-        return;
-    }
-    Eight<T> e[CHUNKS];
+        const float tail = last < vocab ? to_float<T>(l[last]) : -INFINITY;
+        // The token's logit goes into the maximum: it is there before the row's first barrier, and the gradient may be written over the row
+        // behind it.
+        const float chosen = to_float<T>(l[w.token]);
+        float top = fmaxf(chosen, tail);
 #pragma unroll
-    for (int c = 0; c < CHUNKS; ++c) {
-        const int64_t i = (c * LANES + lane) * 8;
-        load_some(e[c], l + i, a.vocab - i, NONE);
-    }
-    // The token's logit goes into the maximum: it is there before the row's first barrier, and the gradient may be written over the row
-    // behind it.
-    const float chosen = to_float<T>(l[token]);
-    float top = chosen;
+        for (int c = 0; c < CHUNKS; ++c) {
+            if (c < chunks) {
 #pragma unroll
-    for (int c = 0; c < CHUNKS; ++c)
-#pragma unroll
-        for (int k = 0; k < 8; ++k) top = fmaxf(top, e[c][k]);
-    top = over_row<Max, LANES>(top, tops);
-    const Exponent x(top);
-    float sum = 0.0f;
-#pragma unroll
-    for (int c = 0; c < CHUNKS; ++c)
-#pragma unroll
-        for (int k = 0; k < 8; ++k) sum += x.of(e[c][k]);
-    sum = over_row<Add, LANES>(sum, sums);
-    const float logp = (chosen - top) - x.log_sum(sum, top);
-    float2 f = make_float2(0.0f, 0.0f);
-    if (a.loss) f = row_loss(a, row, q, logp);
-    if (lane == 0) {
-        if (a.logp) a.logp[row] = logp;
-        if (a.losses) a.losses[row] = f.x;
-    }
-    if (!g) return;
-    const float p = -f.y / sum;
-#pragma unroll
-    for (int c = 0; c < CHUNKS; ++c) {
-        const int64_t i = (c * LANES + lane) * 8;
-        float v[8];
-#pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] = x.of(e[c][k]) * p;
-        if ((uint64_t)(token - i) < 8u) {
-#pragma unroll
-            for (int k = 0; k < 8; ++k)
-                if (token - i == k) v[k] += f.y;
+                for (int k = 0; k < 8; ++k) top = fmaxf(top, e[c][k]);
+            }
+            __builtin_amdgcn_sched_barrier(0);
         }
-        Eight<T> o;
-        o.round(v);
-        store_some(o, g + i, a.vocab - i);
+        top = over_row<Max, LANES>(top, tops);
+        const Exponent x(top);
+        float sum = x.of(tail);
+#pragma unroll
+        for (int c = 0; c < CHUNKS; ++c) {
+            if (c < chunks) {
+                float v[8];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) v[k] = x.of(e[c][k]);
+                sum += ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        sum = over_row<Add, LANES>(sum, sums);
+        // The row's own arithmetic is one wavefront's: a hundred instructions that sixteen need not repeat.
+        float2 f = make_float2(0.0f, 0.0f);
+        if (LANES <= 64 || threadIdx.x < 64) {
+            const float logp = (chosen - top) - x.log_sum(sum, top);
+            if (a.loss) f = row_loss(a, w, logp);
+            if (lane == 0) {
+                if (a.logp) a.logp[row] = logp;
+                if (a.losses) a.losses[row] = f.x;
+                if (LANES > 64) slope = f.y;
+            }
+        }
+        if (!a.dlogits) continue;
+        if (LANES > 64) {
+            __syncthreads();
+            f.y = slope;
+        }
+        T *g = static_cast<T *>(a.dlogits) + row * a.dlogits_stride;
+        const float p = -f.y / sum;
+#pragma unroll
+        for (int c = 0; c < CHUNKS; ++c) {
+            if (c < chunks) {
+                const int i = (c * LANES + lane) * 8;
+                float v[8];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) v[k] = x.of(e[c][k]) * p;
+                const int at = (int)w.token - part.head - i;
+                if ((unsigned)at < 8u) {
+#pragma unroll
+                    for (int k = 0; k < 8; ++k)
+                        if (at == k) v[k] += f.y;
+                }
+                Eight<T> o;
+                o.round(v);
+                if (i < whole) o.store_at(g + part.head + c * LANES * 8, off);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        if (last < vocab) g[last] = from_float<T>(x.of(tail) * p + (w.token == last ? f.y : 0.0f));
     }
 }
 
@@ -150,20 +229,13 @@ __global__ __launch_bounds__(LONG_THREADS) void k_policy_long(PolicyArgs a)
     const int64_t row = blockIdx.x;
     const T *l = static_cast<const T *>(a.logits) + row * a.stride;
     T *g = a.dlogits ? static_cast<T *>(a.dlogits) + row * a.dlogits_stride : nullptr;
-    const int64_t token = a.tokens[row];
-    const float q = row_weight(a, row, token);
-    if (q == 0.0f) {
-        if (threadIdx.x == 0) {
-            if (a.logp) a.logp[row] = 0.0f;
-            if (a.losses) a.losses[row] = 0.0f;
-        }
-        if (g) {
-            Eight<T> zero;
-            zero.fill(0u);
-            for (int64_t i = (int64_t)threadIdx.x * 8; i < a.vocab; i += LONG_THREADS * 8) store_some(zero, g + i, a.vocab - i);
-        }
+    RowArgs w;
+    w.load(a, row);
+    if (w.masked(a)) {
+        masked_row<T, LONG_THREADS>(a, row, threadIdx.x);
         return;
     }
+    const int64_t token = w.token;
     const float chosen = to_float<T>(l[token]);
     // sum of 2^((l - top) * L) so far; a thread that has seen nothing but -inf has top = -inf and sum 0
     float top = -INFINITY, sum = 0.0f;
@@ -193,7 +265,7 @@ __global__ __launch_bounds__(LONG_THREADS) void k_policy_long(PolicyArgs a)
     if (all == -INFINITY) sum = NAN;        // nothing but -inf
     const float logp = (chosen - all) - logf(sum);
     float2 f = make_float2(0.0f, 0.0f);
-    if (a.loss) f = row_loss(a, row, q, logp);
+    if (a.loss) f = row_loss(a, w, logp);
     if (threadIdx.x == 0) {
         if (a.logp) a.logp[row] = logp;
         if (a.losses) a.losses[row] = f.x;
@@ -215,12 +287,18 @@ __global__ __launch_bounds__(LONG_THREADS) void k_policy_long(PolicyArgs a)
     }
 }
 
-// loss <- the sum of the rows' losses: thread t adds rows t, t + 1024, ..., then a fixed tree.
+// loss <- the sum of the rows' losses: thread t adds rows t, t + 1024, ..., eight of them on their way at once, then a fixed tree.
 __global__ __launch_bounds__(1024) void k_sum_losses(const float *losses, int64_t rows, float *loss)
 {
     __shared__ double sums[1024];
     double s = 0.0;
-    for (int64_t i = threadIdx.x; i < rows; i += 1024) s += (double)losses[i];
+    for (int64_t i = threadIdx.x; i < rows; i += 8 * 1024) {
+        float v[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = i + k * 1024 < rows ? losses[i + k * 1024] : 0.0f;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) s += (double)v[k];
+    }
     sums[threadIdx.x] = s;
     __syncthreads();
     for (int h = 512; h > 0; h /= 2) {

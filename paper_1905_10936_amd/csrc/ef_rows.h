@@ -23,7 +23,14 @@ typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
-// Eight elements as they lie in memory.
+// An offset that is 32 bits wide where it is used: an access then adds it to a scalar base itself.
+__device__ __forceinline__ unsigned here(unsigned off)
+{
+    asm volatile("" : "+v"(off));
+    return off;
+}
+
+// Eight elements as they lie in memory.  load_at, store_at: at a base that is the same for the wavefront and a lane's bytes from there.
 template <class T>
 struct Eight;
 template <>
@@ -31,6 +38,8 @@ struct Eight<bf16_t> {
     u32x4 w;
     __device__ __forceinline__ void load(const bf16_t *p) { w = *reinterpret_cast<const u32x4_any *>(p); }
     __device__ __forceinline__ void store(bf16_t *p) const { *reinterpret_cast<u32x4_any *>(p) = w; }
+    __device__ __forceinline__ void load_at(const void *base, unsigned off) { w = *(const EF_GLOBAL u32x4_any *)((const EF_GLOBAL char *)base + here(off)); }
+    __device__ __forceinline__ void store_at(void *base, unsigned off) const { *(EF_GLOBAL u32x4_any *)((EF_GLOBAL char *)base + here(off)) = w; }
     __device__ __forceinline__ void fill(unsigned two) { w = u32x4{two, two, two, two}; }
     __device__ __forceinline__ float operator[](int i) const
     {
@@ -62,6 +71,18 @@ struct Eight<float> {
     {
         *reinterpret_cast<u32x4_word *>(p) = lo;
         *reinterpret_cast<u32x4_word *>(p + 4) = hi;
+    }
+    __device__ __forceinline__ void load_at(const void *base, unsigned off)
+    {
+        const EF_GLOBAL char *p = (const EF_GLOBAL char *)base + here(off);
+        lo = *(const EF_GLOBAL u32x4_word *)p;
+        hi = *(const EF_GLOBAL u32x4_word *)(p + 16);
+    }
+    __device__ __forceinline__ void store_at(void *base, unsigned off) const
+    {
+        EF_GLOBAL char *p = (EF_GLOBAL char *)base + here(off);
+        *(EF_GLOBAL u32x4_word *)p = lo;
+        *(EF_GLOBAL u32x4_word *)(p + 16) = hi;
     }
     __device__ __forceinline__ void fill(unsigned one) { lo = hi = u32x4{one, one, one, one}; }
     __device__ __forceinline__ float operator[](int i) const { return __uint_as_float(i < 4 ? lo[i & 3] : hi[i & 3]); }
@@ -105,6 +126,13 @@ template <>
 __device__ __forceinline__ float to_float<float>(float v) { return v; }
 template <>
 __device__ __forceinline__ float to_float<bf16_t>(bf16_t v) { return __uint_as_float((unsigned)v.bits << 16); }
+
+template <class T>
+__device__ __forceinline__ T from_float(float v);
+template <>
+__device__ __forceinline__ float from_float<float>(float v) { return v; }
+template <>
+__device__ __forceinline__ bf16_t from_float<bf16_t>(float v) { return bf16_t{__builtin_bit_cast(uint16_t, (__bf16)v)}; }
 
 // The first `left` (any number, also none or less) of eight elements at p; `other` (a bit pattern; bf16: twice) for the rest.
 template <class T>
@@ -175,9 +203,12 @@ __device__ __forceinline__ float over_row(float v, float *at)
         v = over_lanes<Op, 64>(v);
         if (threadIdx.x % 64 == 0) at[threadIdx.x / 64] = v;
         __syncthreads();
-        v = at[0];
-#pragma unroll
-        for (int i = 1; i < LANES / 64; ++i) v = Op::of(v, at[i]);
+        // 4, 8 or 16 wavefronts: each lane takes one of their results, the lanes of a row of 16 then have all of them
+        v = at[threadIdx.x % (LANES / 64)];
+        v = Op::of(v, lane_move<DPP_XOR1>(v));
+        v = Op::of(v, lane_move<DPP_XOR2>(v));
+        if constexpr (LANES >= 512) v = Op::of(v, lane_move<DPP_HALF_MIRROR>(v));
+        if constexpr (LANES >= 1024) v = Op::of(v, lane_move<DPP_MIRROR>(v));
         return v;
     }
 }
