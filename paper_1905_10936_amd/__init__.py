@@ -84,6 +84,7 @@ def _load_native(L):
             raise RuntimeError("it is built for %s, this is %s: run paper_1905_10936_amd/build.py" %
                                (module.built_for, _build.binding_built_for()))
         module.bind(*(ctypes.cast(getattr(L, name), ctypes.c_void_p).value for name in _NATIVE_CALLS))
+        module.bind_layers(*(ctypes.cast(getattr(L, name), ctypes.c_void_p).value for name in layers.NATIVE_CALLS))
     except Exception as e:              # no compiler, another torch or Python, an old file: calls take 1 to 3 us longer
         import warnings
         warnings.warn("%s cannot be used, calls go through ctypes: %s" % (os.path.basename(_build.BINDING), e), RuntimeWarning)

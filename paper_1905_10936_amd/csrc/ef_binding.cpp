@@ -34,6 +34,17 @@ struct Entries {
     decltype(&ef_compressor_quality) compressor_quality;
 } F;
 
+// The operators of a worker's forward and backward pass (bind_layers).
+struct LayerEntries {
+    decltype(&ef_act_encode) act_encode;
+    decltype(&ef_act_decode) act_decode;
+    decltype(&ef_norm_forward) norm_forward;
+    decltype(&ef_norm_backward) norm_backward;
+    decltype(&ef_weight_grad) weight_grad;
+    decltype(&ef_token_logp) token_logp;
+    decltype(&ef_policy_loss) policy_loss;
+} G;
+
 // What a Plan or a State knows about itself, packed by Python (no bytes: it is closed).
 struct PlanKey {
     ef_plan *plan;
@@ -42,6 +53,17 @@ struct PlanKey {
 struct StateKey {
     ef_state *state;
     int64_t n;
+};
+struct WorkspaceKey {
+    ef_workspace *workspace;
+    int64_t max_rows;
+};
+
+// A matrix argument of the layers: rows of `width` contiguous elements, `stride` apart; no tensor: p is null.
+struct Mat {
+    void *p = nullptr;
+    int64_t rows = 0, width = 0, stride = 0;
+    at::ScalarType type = at::kFloat;
 };
 
 // Arguments one after the other; `ok` is false from the first one on that is not as expected.
@@ -76,6 +98,59 @@ public:
         return t;
     }
     const at::Tensor *floats() { return tensor(at::kFloat); }
+    // a 1-D tensor (one row) or a 2-D one of either type, its rows contiguous, on the GPU
+    Mat matrix()
+    {
+        Mat m;
+        PyObject *o = next();
+        ok = ok && THPVariable_CheckExact(o);
+        if (!ok) return m;
+        const at::Tensor &t = THPVariable_Unpack(o);
+        ok = t.defined() && t.is_cuda() && (t.dim() == 1 || t.dim() == 2) && (t.scalar_type() == at::kFloat || t.scalar_type() == at::kBFloat16);
+        if (!ok) return m;
+        m.type = t.scalar_type();
+        m.rows = t.dim() == 1 ? 1 : t.size(0);
+        m.width = t.size(-1);
+        m.stride = t.dim() == 1 ? m.width : t.stride(0);
+        ok = m.width < 2 || t.stride(-1) == 1;
+        m.p = t.data_ptr();
+        return m;
+    }
+    // the same or None, of another matrix's shape and type
+    Mat matrix_like(const Mat &m)
+    {
+        if (ok && a_[i_] == Py_None) {
+            ++i_;
+            return Mat();
+        }
+        const Mat r = matrix();
+        ok = ok && r.rows == m.rows && r.width == m.width && r.type == m.type;
+        return r;
+    }
+    // a contiguous tensor of n entries, or None
+    void *vector(at::ScalarType type, int64_t n)
+    {
+        if (ok && a_[i_] == Py_None) {
+            ++i_;
+            return nullptr;
+        }
+        const at::Tensor *t = tensor(type);
+        ok = ok && t->numel() == n;
+        return ok ? t->data_ptr() : nullptr;
+    }
+    float *row_floats(int64_t n) { return static_cast<float *>(vector(at::kFloat, n)); }
+    // a checkpoint of rows of `width`, or None
+    void *act(int64_t rows, int64_t width)
+    {
+        const int64_t groups = (width + 31) / 32;
+        return vector(at::kByte, (rows * groups * 33 + 15) / 16 * 16);
+    }
+    int flag()
+    {
+        PyObject *o = next();
+        ok = ok && (o == Py_True || o == Py_False);
+        return ok && o == Py_True;
+    }
     float number()
     {
         PyObject *o = next();
@@ -359,10 +434,129 @@ PyObject *compressor_quality(PyObject *, PyObject *const *a, Py_ssize_t n)
     });
 }
 
-// bind(addresses): the entry points' addresses, in the order of Entries.
-PyObject *bind(PyObject *, PyObject *const *a, Py_ssize_t n)
+int type_of(const Mat &m) { return m.type == at::kBFloat16 ? EF_TYPE_BF16 : EF_TYPE_FP32; }
+
+PyObject *act_encode(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
-    constexpr Py_ssize_t count = sizeof(Entries) / sizeof(void *);
+    return call(a, n, 3, [](Args &x) {
+        const Mat m = x.matrix();
+        void *const act = x.act(m.rows, m.width);
+        void *const s = x.stream();
+        if (!x.ok) return 0;
+        return unlocked([&] { return G.act_encode(m.rows, m.width, type_of(m), m.p, m.stride, act, s); });
+    });
+}
+
+PyObject *act_decode(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return call(a, n, 3, [a, n](Args &x) {
+        if (n != 3) return 0;
+        Args last(a + 1, 1, 1);
+        const Mat m = last.matrix();
+        x.need(last.ok);
+        void *const act = x.act(m.rows, m.width);
+        x.matrix();
+        void *const s = x.stream();
+        if (!x.ok) return 0;
+        return unlocked([&] { return G.act_decode(m.rows, m.width, act, type_of(m), m.p, m.stride, s); });
+    });
+}
+
+PyObject *norm_forward(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return call(a, n, 9, [](Args &x) {
+        const Mat m = x.matrix(), r = x.matrix_like(m);
+        const float *weight = x.row_floats(m.width);
+        const float eps = x.number();
+        const Mat h = x.matrix_like(m), y = x.matrix_like(m);
+        void *const act = x.act(m.rows, m.width);
+        float *const rstd = x.row_floats(m.rows);
+        void *const s = x.stream();
+        if (!x.ok) return 0;
+        return unlocked([&] {
+            return G.norm_forward(m.rows, m.width, type_of(m), m.p, m.stride, r.p, r.stride, weight, eps, h.p, h.stride, y.p, y.stride, act, rstd, s);
+        });
+    });
+}
+
+PyObject *norm_backward(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return call(a, n, 10, [](Args &x) {
+        const WorkspaceKey k = x.key<WorkspaceKey>();
+        const Mat m = x.matrix();
+        const void *act = x.act(m.rows, m.width);
+        const float *rstd = x.row_floats(m.rows), *weight = x.row_floats(m.width);
+        const Mat dh = x.matrix_like(m), dx = x.matrix_like(m);
+        float *const dweight = x.row_floats(m.width);
+        const int accumulate = x.flag();
+        void *const s = x.stream();
+        if (!x.ok) return 0;
+        return unlocked([&] {
+            return G.norm_backward(k.workspace, m.rows, m.width, type_of(m), m.p, m.stride, act, rstd, weight, dh.p, dh.stride, dx.p, dx.stride, dweight,
+                                   accumulate, s);
+        });
+    });
+}
+
+PyObject *weight_grad(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return call(a, n, 7, [a, n](Args &x) {
+        if (n != 7) return 0;
+        Args fifth(a + 4, 1, 1);
+        const at::Tensor *dw = fifth.floats();
+        x.need(fifth.ok && dw->dim() == 2);
+        if (!x.ok) return 0;
+        const int64_t width = dw->size(1);
+        const WorkspaceKey k = x.key<WorkspaceKey>();
+        const Mat m = x.matrix();
+        x.need(m.width == dw->size(0));
+        const void *act = x.act(m.rows, width);
+        const float *scale = x.row_floats(width);
+        x.floats();
+        const int accumulate = x.flag();
+        void *const s = x.stream();
+        if (!x.ok) return 0;
+        float *const out = f32(dw);
+        return unlocked([&] { return G.weight_grad(k.workspace, m.rows, m.width, width, type_of(m), m.p, m.stride, act, scale, out, accumulate, s); });
+    });
+}
+
+PyObject *token_logp(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return call(a, n, 4, [](Args &x) {
+        const Mat m = x.matrix();
+        const int64_t *tokens = static_cast<const int64_t *>(x.vector(at::kLong, m.rows));
+        float *const logp = x.row_floats(m.rows);
+        void *const s = x.stream();
+        if (!x.ok) return 0;
+        return unlocked([&] { return G.token_logp(m.rows, m.width, type_of(m), m.p, m.stride, tokens, logp, s); });
+    });
+}
+
+PyObject *policy_loss(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return call(a, n, 15, [](Args &x) {
+        const WorkspaceKey k = x.key<WorkspaceKey>();
+        const Mat m = x.matrix();
+        const int64_t *tokens = static_cast<const int64_t *>(x.vector(at::kLong, m.rows));
+        const float *old = x.row_floats(m.rows), *ref = x.row_floats(m.rows), *advantage = x.row_floats(m.rows), *weight = x.row_floats(m.rows);
+        const float low = x.number(), high = x.number(), kl = x.number();
+        float *const logp = x.row_floats(m.rows), *const losses = x.row_floats(m.rows), *const loss = x.row_floats(1);
+        const Mat g = x.matrix_like(m);
+        void *const s = x.stream();
+        if (!x.ok) return 0;
+        return unlocked([&] {
+            return G.policy_loss(k.workspace, m.rows, m.width, type_of(m), m.p, m.stride, tokens, old, ref, advantage, weight, low, high, kl, logp, losses,
+                                 loss, g.p, g.stride, s);
+        });
+    });
+}
+
+// bind(addresses), bind_layers(addresses): the entry points' addresses, in the order of Entries and of LayerEntries.
+template <class Table>
+PyObject *fill(Table &table, PyObject *const *a, Py_ssize_t n)
+{
+    constexpr Py_ssize_t count = sizeof(Table) / sizeof(void *);
     void *p[count];
     if (n != count) {
         PyErr_SetString(PyExc_TypeError, "bind: one address for each entry point");
@@ -375,9 +569,11 @@ PyObject *bind(PyObject *, PyObject *const *a, Py_ssize_t n)
             return nullptr;
         }
     }
-    memcpy(&F, p, sizeof F);
+    memcpy(&table, p, sizeof table);
     Py_RETURN_NONE;
 }
+PyObject *bind(PyObject *, PyObject *const *a, Py_ssize_t n) { return fill(F, a, n); }
+PyObject *bind_layers(PyObject *, PyObject *const *a, Py_ssize_t n) { return fill(G, a, n); }
 
 #define EF_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {EF_METHOD(bind),
@@ -392,6 +588,14 @@ PyMethodDef methods[] = {EF_METHOD(bind),
                          EF_METHOD(apply_wd),
                          EF_METHOD(apply_fused),
                          EF_METHOD(compressor_quality),
+                         EF_METHOD(bind_layers),
+                         EF_METHOD(act_encode),
+                         EF_METHOD(act_decode),
+                         EF_METHOD(norm_forward),
+                         EF_METHOD(norm_backward),
+                         EF_METHOD(weight_grad),
+                         EF_METHOD(token_logp),
+                         EF_METHOD(policy_loss),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_ef_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -131,11 +131,11 @@ __global__ __launch_bounds__(policy_threads(LANES), LANES == 1024 && sizeof(T) *
     const int lane = threadIdx.x % LANES, vocab = (int)a.vocab;
     const unsigned off = lane * 8 * (unsigned)sizeof(T);
     const int64_t teams = (int64_t)gridDim.x * TEAMS;
-    int64_t row = (int64_t)blockIdx.x * TEAMS + (TEAMS > 1 ? (int)__builtin_amdgcn_readfirstlane(threadIdx.x / LANES) : 0);
+    int64_t row = (int64_t)blockIdx.x * TEAMS + (LANES < 64 ? (int)threadIdx.x / LANES : LANES < 256 ? (int)__builtin_amdgcn_readfirstlane(threadIdx.x / LANES) : 0);
     RowArgs next;
     if (row < a.rows) next.load(a, row);
     for (; row < a.rows; row += teams) {
-        const RowArgs w = next.scalar();
+        const RowArgs w = LANES >= 64 ? next.scalar() : next;
         if (row + teams < a.rows) next.load(a, row + teams);
         if (w.masked(a)) {
             masked_row<T, LANES>(a, row, lane);

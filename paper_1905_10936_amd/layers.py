@@ -7,6 +7,7 @@ slices of a flat vector.
 """
 import ctypes
 import struct
+import sys
 
 import torch
 
@@ -14,6 +15,9 @@ from . import _check, _f32, _ptr, _stream_ptr, _u8, lib
 
 EF_TYPE_FP32, EF_TYPE_BF16 = 0, 1
 EF_NORM_MAX_WIDTH = 16384
+# what csrc/ef_binding.cpp marshals, in the order of its LayerEntries
+NATIVE_CALLS = ("ef_act_encode", "ef_act_decode", "ef_norm_forward", "ef_norm_backward", "ef_weight_grad", "ef_token_logp", "ef_policy_loss")
+_package = sys.modules[__package__]     # whose _native is the binding, once it is loaded
 _TYPES = {torch.float32: EF_TYPE_FP32, torch.bfloat16: EF_TYPE_BF16}
 
 
@@ -87,6 +91,9 @@ def _act(t, rows, width, name="act"):
 
 def ef_act_encode(x, act, stream=None):
     """act: uint8 [ef_act_bytes(rows, width)] <- checkpoint of x [rows][width]."""
+    rc = _package._native.act_encode(x, act, stream)
+    if rc is not None:
+        return _check(rc)
     rows, width = _rows(x, "x")
     xp, xs = _matrix(x, (rows, width), x.dtype, "x")
     _check(lib().ef_act_encode(rows, width, _type(x, "x"), xp, xs, _act(act, rows, width), _stream_ptr(stream)))
@@ -94,6 +101,9 @@ def ef_act_encode(x, act, stream=None):
 
 def ef_act_decode(act, y, stream=None):
     """y [rows][width] <- what the checkpoint of such a matrix stands for."""
+    rc = _package._native.act_decode(act, y, stream)
+    if rc is not None:
+        return _check(rc)
     rows, width = _rows(y, "y")
     yp, ys = _matrix(y, (rows, width), y.dtype, "y")
     _check(lib().ef_act_decode(rows, width, _act(act, rows, width), _type(y, "y"), yp, ys, _stream_ptr(stream)))
@@ -102,6 +112,9 @@ def ef_act_decode(act, y, stream=None):
 def ef_norm_forward(x, residual, weight, eps, h, y, act, rstd, stream=None):
     """h <- x + residual; y <- norm(x + residual) * weight; act <- checkpoint of the norm; rstd float32 [rows].
     residual, weight (float32 [width]) and any of the outputs but one may be None."""
+    rc = _package._native.norm_forward(x, residual, weight, eps, h, y, act, rstd, stream)
+    if rc is not None:
+        return _check(rc)
     shape = _rows(x, "x")
     (xp, xs), (rp, rs) = _matrix(x, shape, x.dtype, "x"), _matrix(residual, shape, x.dtype, "residual")
     (hp, hs), (yp, ys) = _matrix(h, shape, x.dtype, "h"), _matrix(y, shape, x.dtype, "y")
@@ -140,31 +153,50 @@ def ef_workspace_destroy(workspace):
     workspace.close()
 
 
+def _key(workspace):
+    return workspace._key if type(workspace) is Workspace else b""
+
+
+def _handle(workspace):
+    if not isinstance(workspace, Workspace):
+        raise TypeError("workspace must be what ef_workspace_create gives")
+    return workspace._h
+
+
 def ef_norm_backward(workspace, dy, act, rstd, weight, dh, dx, dweight, accumulate=False, stream=None):
     """dx <- gradient of the norm's input from dy and (dh, or None) that of its residual path; dweight (float32
     [width], or None) <- or += the weight's."""
+    rc = _package._native.norm_backward(_key(workspace), dy, act, rstd, weight, dh, dx, dweight, accumulate, stream)
+    if rc is not None:
+        return _check(rc)
     shape = _rows(dy, "dy")
     (gp, gs), (hp, hs) = _matrix(dy, shape, dy.dtype, "dy"), _matrix(dh, shape, dy.dtype, "dh")
     xp, xs = _matrix(dx, shape, dy.dtype, "dx")
-    _check(lib().ef_norm_backward(workspace._h, shape[0], shape[1], _type(dy, "dy"), gp, gs, _act(act, *shape),
+    _check(lib().ef_norm_backward(_handle(workspace), shape[0], shape[1], _type(dy, "dy"), gp, gs, _act(act, *shape),
                                   _vector(rstd, shape[0], _f32, "rstd"), _vector(weight, shape[1], _f32, "weight"), hp, hs, xp, xs,
                                   _vector(dweight, shape[1], _f32, "dweight"), int(bool(accumulate)), _stream_ptr(stream)))
 
 
 def ef_weight_grad(workspace, dz, act, column_scale, dw, accumulate=False, stream=None):
     """dw [out][width] (float32) <- or += dz^T times what act stands for, columns times column_scale (float32 [width], or None)."""
+    rc = _package._native.weight_grad(_key(workspace), dz, act, column_scale, dw, accumulate, stream)
+    if rc is not None:
+        return _check(rc)
     rows, out = _rows(dz, "dz")
     if not isinstance(dw, torch.Tensor) or dw.dim() != 2 or dw.shape[0] != out:
         raise TypeError("dw must be 2-D, %d x width" % out)
     width = dw.shape[1]
     zp, zs = _matrix(dz, (rows, out), dz.dtype, "dz")
-    _check(lib().ef_weight_grad(workspace._h, rows, out, width, _type(dz, "dz"), zp, zs, _act(act, rows, width),
+    _check(lib().ef_weight_grad(_handle(workspace), rows, out, width, _type(dz, "dz"), zp, zs, _act(act, rows, width),
                                 _vector(column_scale, width, _f32, "column_scale"), _ptr(dw, _f32, "dw"), int(bool(accumulate)),
                                 _stream_ptr(stream)))
 
 
 def ef_token_logp(logits, tokens, logp, stream=None):
     """logp float32 [rows] <- log-probabilities of tokens (int64 [rows]) under softmax(logits [rows][vocab])."""
+    rc = _package._native.token_logp(logits, tokens, logp, stream)
+    if rc is not None:
+        return _check(rc)
     shape = _rows(logits, "logits")
     lp, ls = _matrix(logits, shape, logits.dtype, "logits")
     _check(lib().ef_token_logp(shape[0], shape[1], _type(logits, "logits"), lp, ls, _vector(tokens, shape[0], torch.int64, "tokens"),
@@ -175,10 +207,14 @@ def ef_policy_loss(workspace, logits, tokens, logp_old, logp_ref, advantage, tok
                    dlogits, stream=None):
     """Clipped policy loss with a KL term: logp, losses (float32 [rows]), loss (float32 [1]) and dlogits (like logits, or
     logits itself); any of the outputs but one, and logp_old, logp_ref and token_weight, may be None."""
+    rc = _package._native.policy_loss(_key(workspace), logits, tokens, logp_old, logp_ref, advantage, token_weight, clip_low, clip_high, kl, logp,
+                                       losses, loss, dlogits, stream)
+    if rc is not None:
+        return _check(rc)
     shape = _rows(logits, "logits")
     n = shape[0]
     (lp, ls), (gp, gs) = _matrix(logits, shape, logits.dtype, "logits"), _matrix(dlogits, shape, logits.dtype, "dlogits")
-    _check(lib().ef_policy_loss(workspace._h, n, shape[1], _type(logits, "logits"), lp, ls, _vector(tokens, n, torch.int64, "tokens"),
+    _check(lib().ef_policy_loss(_handle(workspace), n, shape[1], _type(logits, "logits"), lp, ls, _vector(tokens, n, torch.int64, "tokens"),
                                 _vector(logp_old, n, _f32, "logp_old"), _vector(logp_ref, n, _f32, "logp_ref"),
                                 _vector(advantage, n, _f32, "advantage"), _vector(token_weight, n, _f32, "token_weight"), float(clip_low),
                                 float(clip_high), float(kl), _vector(logp, n, _f32, "logp"), _vector(losses, n, _f32, "losses"),

@@ -118,9 +118,10 @@ def policy(logits, tokens, old, ref, adv, weight, low, high, kl):
         with np.errstate(invalid="ignore"):
             e = np.exp(logits[t] - top)
         s = e.sum()
-        logp[t] = logits[t, a] - top - math.log(s)
-        # exponents are off by their own rounding: of the terms that weigh, a few tens at most
-        off[0][t] = tol + 4 * EPS * (abs(logits[t, a] - top) + math.log(s) + 16)
+        with np.errstate(invalid="ignore"):
+            logp[t] = logits[t, a] - top - math.log(s)
+            # exponents are off by their own rounding: of the terms that weigh, a few tens at most
+            off[0][t] = tol + 4 * EPS * (abs(logits[t, a] - top) + math.log(s) + 16)
         if adv is None:
             continue
         r = 1.0 if old is None else math.exp(logp[t] - old[t])

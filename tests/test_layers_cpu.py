@@ -133,3 +133,31 @@ def test_the_binding_says_what_is_wrong():
         ef.ef_weight_grad(None, x, act, None, torch.zeros(12))
     with pytest.raises(TypeError, match="tensor"):
         ef.ef_token_logp([1.0], None, None)
+    x2 = torch.zeros(4, 8)
+    with pytest.raises(TypeError, match="CUDA"):
+        ef.ef_weight_grad(None, x2, act, None, torch.zeros(8, 8))
+
+
+def test_the_native_calls_leave_what_they_cannot_vouch_for():
+    """Without a GPU nothing is taken, whatever its place; the calls have as many arguments as their wrappers."""
+    import inspect
+    import os
+    import struct
+
+    from paper_1905_10936_amd import build, layers
+    ef.lib()
+    if not os.path.exists(build.BINDING):
+        pytest.skip("ef_binding.cpp could not be built here")
+    t, v, act, key = torch.zeros(4, 8), torch.zeros(4), torch.zeros(ef.ef_act_bytes(4, 8), dtype=torch.uint8), struct.pack("Pq", 0, 4)
+    tokens = torch.zeros(4, dtype=torch.int64)
+    calls = {"act_encode": (t, act), "act_decode": (act, t), "norm_forward": (t, None, None, 0.1, None, t, act, v),
+             "norm_backward": (key, t, act, v, None, None, t, None, False), "weight_grad": (key, t, act, None, t, False),
+             "token_logp": (t, tokens, v), "policy_loss": (key, t, tokens, v, v, v, v, 0.1, 0.1, 0.1, v, v, None, t)}
+    assert ["ef_" + name for name in calls] == list(layers.NATIVE_CALLS)
+    for name, args in calls.items():
+        call = getattr(ef._native, name)
+        assert len(args) + 1 == len(inspect.signature(getattr(ef, "ef_" + name)).parameters), name
+        assert call(*args, None) is None and call(*args) is None and call() is None, name
+        assert call(*(None for _ in args), None) is None, name
+    with pytest.raises(TypeError):
+        ef._native.bind_layers(1)
