@@ -163,6 +163,19 @@ void policy_rows(const ef::PolicyArgs &a, hipStream_t s)
         }
 }
 
+template <class T>
+void policy_slices(const ef::PolicyArgs &a, float *parts, float *loss, hipStream_t s)
+{
+    ef::SliceRef r;
+    r.joint = reinterpret_cast<float2 *>(parts);
+    r.chosen = parts + 2 * ef::SLICED_ROWS * ef::SLICES_MAX;
+    r.count = (int)std::min<int64_t>(ceil_div(a.vocab, ef::SLICE), ef::SLICES_MAX);
+    r.length = (int)(ceil_div(a.vocab, r.count * 8) * 8);
+    const dim3 grid((unsigned)(a.rows * r.count));
+    hipLaunchKernelGGL(ef::k_policy_slices<T>, grid, dim3(ef::SLICE_THREADS), 0, s, a, r);
+    hipLaunchKernelGGL(ef::k_policy_join<T>, dim3(grid.x + (loss ? 1u : 0u)), dim3(ef::SLICE_THREADS), 0, s, a, r, loss);
+}
+
 int policy_args(int64_t rows, int64_t vocab, int type, const void *logits, int64_t stride, const int64_t *tokens)
 {
     if (!logits || !tokens) return EF_ERR_NULL;
@@ -460,6 +473,11 @@ int ef_policy_loss(ef_workspace *workspace, int64_t rows, int64_t vocab, int typ
     if (rows) {
         const ef::PolicyArgs a{rows, vocab, logits, stride, tokens, logp_old, logp_ref, advantage, token_weight, 1.0f - clip_low,
                                1.0f + clip_high, kl, logp, row_losses, dlogits, dlogits_stride, 1};
+        if (rows <= ef::SLICED_ROWS && vocab > ef::SLICED_VOCAB) {
+            EF_BY_TYPE(type, T, policy_slices<T>(a, workspace->parts, loss, s));
+            EF_HIP(hipGetLastError());
+            return EF_OK;
+        }
         EF_BY_TYPE(type, T, policy_rows<T>(a, s));
         EF_HIP(hipGetLastError());
     }

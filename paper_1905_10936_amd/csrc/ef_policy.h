@@ -219,6 +219,30 @@ __global__ __launch_bounds__(policy_threads(LANES), LANES == 1024 && sizeof(T) *
     }
 }
 
+// Eight more elements to a maximum and the sum of 2^((l - maximum) L) up to here; -inf and 0 while there has been nothing but -inf.
+template <class T>
+__device__ __forceinline__ void more_of_row(const Eight<T> &e, float &top, float &sum)
+{
+    float t = top;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) t = fmaxf(t, e[k]);
+    if (t > top) {
+        sum *= __builtin_amdgcn_exp2f((top - t) * LOG2E);
+        top = t;
+    }
+    float s = 0.0f;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) s += __builtin_amdgcn_exp2f((e[k] - top) * LOG2E);
+    if (top != -INFINITY) {
+        sum += s;
+    } else {
+        // nothing but -inf gives NaN here; a NaN among the eight has to show
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            if (e[k] != e[k]) sum = e[k];
+    }
+}
+
 // Rows longer than a workgroup's registers: maximum and sum kept up to date chunk by chunk, the row read again for the gradient.
 constexpr int LONG_THREADS = 1024;
 template <class T>
@@ -242,23 +266,7 @@ __global__ __launch_bounds__(LONG_THREADS) void k_policy_long(PolicyArgs a)
     for (int64_t i = (int64_t)threadIdx.x * 8; i < a.vocab; i += LONG_THREADS * 8) {
         Eight<T> e;
         load_some(e, l + i, a.vocab - i, NONE);
-        float t = top;
-#pragma unroll
-        for (int k = 0; k < 8; ++k) t = fmaxf(t, e[k]);
-        if (t > top) {
-            sum *= __builtin_amdgcn_exp2f((top - t) * LOG2E);
-            top = t;
-        }
-        float s = 0.0f;
-#pragma unroll
-        for (int k = 0; k < 8; ++k) s += __builtin_amdgcn_exp2f((e[k] - top) * LOG2E);
-        if (top != -INFINITY) sum += s;
-        else if (s != s) {
-            // eight times -inf, or NaN among them: the latter has to show
-#pragma unroll
-            for (int k = 0; k < 8; ++k)
-                if (e[k] != e[k]) sum = e[k];
-        }
+        more_of_row(e, top, sum);
     }
     const float all = over_row<Max, LONG_THREADS>(fmaxf(top, chosen), tops);
     sum = over_row<Add, LONG_THREADS>(sum == 0.0f ? 0.0f : sum * __builtin_amdgcn_exp2f((top - all) * LOG2E), sums);
@@ -287,25 +295,196 @@ __global__ __launch_bounds__(LONG_THREADS) void k_policy_long(PolicyArgs a)
     }
 }
 
-// loss <- the sum of the rows' losses: thread t adds rows t, t + 1024, ..., eight of them on their way at once, then a fixed tree.
+// Few rows of many entries: a row cut into slices, a workgroup each, in two kernels.  The first leaves every slice's maximum and sum of exponentials, and the
+// token's logit; in the second each workgroup joins its row's and writes its slice's gradient.  5 rows of 50304 in fp32: 11.8 us with a
+// workgroup to a row, 8.3 with 25; 16 rows of 200000 in bf16: 34.6 and 11.2; 16 of 9000, where a workgroup has its row in registers: 8.0 and 8.3.
+constexpr int SLICE_THREADS = 256, SLICE = 2048, SLICES_MAX = 64, SLICED_ROWS = 64, SLICED_VOCAB = 32768;
+struct SliceRef {
+    float2 *joint;              // [rows][SLICES_MAX] maximum, sum of 2^((l - maximum) L)
+    float *chosen;              // [rows]
+    int count, length;          // slices of a row, elements of one (a multiple of 8)
+};
+
+template <class T>
+__global__ __launch_bounds__(SLICE_THREADS) void k_policy_slices(PolicyArgs a, SliceRef s)
+{
+    __shared__ float tops[SLICE_THREADS / 64], sums[SLICE_THREADS / 64];
+    const int64_t row = blockIdx.x / s.count;
+    const int slice = blockIdx.x % s.count, vocab = (int)a.vocab;
+    RowArgs w;
+    w.load(a, row);
+    if (w.masked(a)) return;
+    const T *l = static_cast<const T *>(a.logits) + row * a.stride;
+    const RowParts part(l, vocab);
+    const int end = min(part.whole, (slice + 1) * s.length), last = slice == 0 ? part.edge(threadIdx.x, vocab) : vocab;
+    float top = last < vocab ? to_float<T>(l[last]) : -INFINITY, sum = top == -INFINITY ? 0.0f : 1.0f;
+    if (top != top) sum = top;
+    for (int i = slice * s.length + (int)threadIdx.x * 8; i < end; i += SLICE_THREADS * 8) {
+        Eight<T> e;
+        e.load(l + part.head + i);
+        more_of_row(e, top, sum);
+    }
+    const float all = over_row<Max, SLICE_THREADS>(top, tops);
+    sum = over_row<Add, SLICE_THREADS>(sum == 0.0f ? 0.0f : sum * __builtin_amdgcn_exp2f((top - all) * LOG2E), sums);
+    if (threadIdx.x == 0) {
+        s.joint[row * SLICES_MAX + slice] = make_float2(all, sum);
+        if (slice == 0) s.chosen[row] = to_float<T>(l[w.token]);
+    }
+}
+
+// Maximum and sum of a row from its slices', one to a lane; all 64 lanes get them.
+__device__ __forceinline__ float2 join_slices(float2 v)
+{
+    const float top = over_lanes<Max, 64>(v.x);
+    const float sum = over_lanes<Add, 64>(v.y == 0.0f ? 0.0f : v.y * __builtin_amdgcn_exp2f((v.x - top) * LOG2E));
+    return make_float2(top, top == -INFINITY ? NAN : sum);      // NaN: nothing but -inf
+}
+__device__ __forceinline__ float2 slice_of(const SliceRef &s, int64_t row, int lane)
+{
+    return lane < s.count ? s.joint[row * SLICES_MAX + lane] : make_float2(-INFINITY, 0.0f);
+}
+
+// The sum of all rows' losses, formed once more from the slices by a workgroup of its own beside those that write the gradient: wavefront w joins
+// rows w, w + 4, ..., whose losses its lanes 0, 1, ... then form at once.
+__device__ __forceinline__ void sum_of_slices(const PolicyArgs &a, const SliceRef &s, float *loss)
+{
+    static_assert(SLICED_ROWS <= 64, "sixteen rows to a wavefront");
+    __shared__ double part[4];
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+    const int64_t mine = wave + 4 * lane;
+    const bool there = lane < 16 && mine < a.rows;
+    RowArgs w;
+    float chosen = 0.0f;
+    if (there) {
+        w.load(a, mine);
+        chosen = s.chosen[mine];
+    }
+    float2 j = make_float2(0.0f, 1.0f);
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+        float2 v[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const int64_t row = wave + 4 * (half * 8 + k);
+            v[k] = row < a.rows ? slice_of(s, row, lane) : make_float2(0.0f, 1.0f);
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const float2 r = join_slices(v[k]);
+            if (lane == half * 8 + k) j = r;
+        }
+    }
+    double total = 0.0;
+    if (there && !w.masked(a)) total = (double)row_loss(a, w, (chosen - j.x) - logf(j.y)).x;
+#pragma unroll
+    for (int h = 8; h > 0; h /= 2) total += __shfl_down(total, h, 16);
+    if (lane == 0) part[wave] = total;
+    __syncthreads();
+    if (threadIdx.x == 0) *loss = (float)((part[0] + part[1]) + (part[2] + part[3]));
+}
+
+template <class T>
+__global__ __launch_bounds__(SLICE_THREADS) void k_policy_join(PolicyArgs a, SliceRef s, float *loss)
+{
+    __shared__ float joined[3];
+    const int64_t row = blockIdx.x / s.count;
+    const int slice = blockIdx.x % s.count, vocab = (int)a.vocab, lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+    if (row == a.rows) {
+        sum_of_slices(a, s, loss);
+        return;
+    }
+    RowArgs w;
+    w.load(a, row);
+    float2 v = make_float2(0.0f, 1.0f);
+    float chosen = 0.0f;
+    if (wave == 0) {
+        v = slice_of(s, row, lane);
+        chosen = s.chosen[row];
+    }
+    const bool masked = w.masked(a);
+    if (wave == 0 && !masked) {
+        const float2 r = join_slices(v);
+        const float logp = (chosen - r.x) - logf(r.y);
+        const float2 f = row_loss(a, w, logp);
+        if (lane == 0) {
+            joined[0] = r.x;
+            joined[1] = r.y;
+            joined[2] = f.y;
+            if (slice == 0) {
+                if (a.logp) a.logp[row] = logp;
+                if (a.losses) a.losses[row] = f.x;
+            }
+        }
+    }
+    if (masked && slice == 0 && threadIdx.x == 0) {
+        if (a.logp) a.logp[row] = 0.0f;
+        if (a.losses) a.losses[row] = 0.0f;
+    }
+    if (!a.dlogits) return;
+    __syncthreads();
+    const T *l = static_cast<const T *>(a.logits) + row * a.stride;
+    T *g = static_cast<T *>(a.dlogits) + row * a.dlogits_stride;
+    const RowParts part(l, vocab);
+    const int end = min(part.whole, (slice + 1) * s.length), last = slice == 0 ? part.edge(threadIdx.x, vocab) : vocab;
+    const float top = masked ? 0.0f : joined[0], c = masked ? 0.0f : joined[2], p = masked ? 0.0f : -c / joined[1];
+    const int token = masked ? -1 : (int)w.token;
+    for (int i = slice * s.length + (int)threadIdx.x * 8; i < end; i += SLICE_THREADS * 8) {
+        float v[8] = {};
+        if (!masked) {
+            Eight<T> e;
+            e.load(l + part.head + i);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                v[k] = __builtin_amdgcn_exp2f((e[k] - top) * LOG2E) * p;
+                if (token - part.head - i == k) v[k] += c;
+            }
+        }
+        Eight<T> o;
+        o.round(v);
+        o.store(g + part.head + i);
+    }
+    if (last < vocab)
+        g[last] = from_float<T>(masked ? 0.0f : __builtin_amdgcn_exp2f((to_float<T>(l[last]) - top) * LOG2E) * p + (token == last ? c : 0.0f));
+}
+
+// loss <- the sum of the rows' losses: a thread adds four neighbouring ones and those 4096 further on, eight times four on their way at once, then a fixed
+// tree.
 __global__ __launch_bounds__(1024) void k_sum_losses(const float *losses, int64_t rows, float *loss)
 {
-    __shared__ double sums[1024];
+    __shared__ double sums[16];
     double s = 0.0;
-    for (int64_t i = threadIdx.x; i < rows; i += 8 * 1024) {
-        float v[8];
+    for (int64_t i = (int64_t)threadIdx.x * 4; i < rows; i += 8 * 4096) {
+        Eight<float> v[4];
+        float e[4] = {};
+        if (i + 7 * 4096 + 4 <= rows) {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] = i + k * 1024 < rows ? losses[i + k * 1024] : 0.0f;
+            for (int k = 0; k < 4; ++k) {
+                v[k].lo = *reinterpret_cast<const u32x4_word *>(losses + i + 2 * k * 4096);
+                v[k].hi = *reinterpret_cast<const u32x4_word *>(losses + i + (2 * k + 1) * 4096);
+            }
 #pragma unroll
-        for (int k = 0; k < 8; ++k) s += (double)v[k];
+            for (int k = 0; k < 4; ++k)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) s += (double)v[k][j];
+        } else {
+            for (int64_t k = i; k < rows; k += 4096) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) e[j] = k + j < rows ? losses[k + j] : 0.0f;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) s += (double)e[j];
+            }
+        }
     }
-    sums[threadIdx.x] = s;
+#pragma unroll
+    for (int h = 32; h > 0; h /= 2) s += __shfl_down(s, h);
+    if (threadIdx.x % 64 == 0) sums[threadIdx.x / 64] = s;
     __syncthreads();
-    for (int h = 512; h > 0; h /= 2) {
-        if ((int)threadIdx.x < h) sums[threadIdx.x] += sums[threadIdx.x + h];
-        __syncthreads();
+    if (threadIdx.x < 16) {
+        s = sums[threadIdx.x];
+#pragma unroll
+        for (int h = 8; h > 0; h /= 2) s += __shfl_down(s, h, 16);
+        if (threadIdx.x == 0) *loss = (float)s;
     }
-    if (threadIdx.x == 0) *loss = (float)sums[0];
 }
 
 }  // namespace ef

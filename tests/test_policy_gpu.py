@@ -74,6 +74,28 @@ def test_loss_and_gradient(vocab, dtype):
     assert np.all(np.abs(logp.double().cpu().numpy() - want[0]) <= want[3][0])
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("vocab", [33000, 41000, 50257, 57345, 70001])
+def test_more_rows_of_large_vocabularies(vocab, dtype):
+    """Beyond the rows that are cut into slices: a workgroup to a row, masked rows among them, also in place."""
+    case = Case(66, vocab, TYPES[dtype], vocab, pad=5)
+    case.tokens[3], case.logits[7] = vocab, float("nan")
+    case.weight[7] = 0.0
+    got = case.run()
+    case.logits[7] = 0.0
+    case.check(got)
+    case.logits[7] = float("nan")
+    assert all(torch.equal(a, b) for a, b in zip(got, case.run(dlogits=lambda logits: logits)))
+
+
+@pytest.mark.parametrize("rows", [1, 7, 33, 64])
+def test_slices(rows):
+    case = Case(rows, 40001, torch.bfloat16, rows, pad=3)
+    got = case.run()
+    case.check(got)
+    assert all(torch.equal(a, b) for a, b in zip(got, case.run(dlogits=lambda logits: logits)))
+
+
 @pytest.mark.parametrize("rows", [1, 2, 255, 1030, 4000])
 def test_rows(rows):
     case = Case(rows, 300, torch.bfloat16, rows)
