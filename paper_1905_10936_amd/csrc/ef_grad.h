@@ -10,9 +10,6 @@
 #pragma once
 #include "ef_rows.h"
 
-#include <type_traits>
-#include <utility>
-
 namespace ef {
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
@@ -220,12 +217,6 @@ struct GradStage {
         }
     }
 };
-
-template <class F, int... I>
-__device__ __forceinline__ void times(F f, std::integer_sequence<int, I...>) { (f(std::integral_constant<int, I>()), ...); }
-// f(0), f(1), ... f(N - 1), the index known to the compiler
-template <int N, class F>
-__device__ __forceinline__ void times(F f) { times(f, std::make_integer_sequence<int, N>()); }
 
 // Eight tokens of a channel to a lane, in two reads of four: lane l gets channel l % 32 and tokens l / 32 * 8 + 0..7 of the 32 channels x 16
 // tokens at p (p: the lane's own place, see grad_lane_offset).

@@ -116,14 +116,18 @@ int launch_norm_backward(ef::NormBackward &a, hipStream_t s)
     return (int)groups;
 }
 
-// The team that holds a row of n: 16 lanes up to 128 channels, a wavefront up to 2048 (no barrier), a workgroup beyond.
+// The team that holds a row of n, with just as many chunks as it takes: 16 lanes up to 128 channels, a wavefront up to 2048 (no barrier), a workgroup
+// beyond.
 #define EF_NORM_TEAM(n, CALL)            \
     ((n) <= 128     ? CALL(16, 1)        \
      : (n) <= 512   ? CALL(64, 1)        \
      : (n) <= 1024  ? CALL(64, 2)        \
+     : (n) <= 1536  ? CALL(64, 3)        \
      : (n) <= 2048  ? CALL(64, 4)        \
      : (n) <= 4096  ? CALL(256, 2)       \
+     : (n) <= 6144  ? CALL(256, 3)       \
      : (n) <= 8192  ? CALL(256, 4)       \
+     : (n) <= 12288 ? CALL(512, 3)       \
                     : CALL(512, 4))
 
 template <class T, int LANES, int CHUNKS>

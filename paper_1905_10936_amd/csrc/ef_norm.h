@@ -2,7 +2,8 @@
 //
 // Both are bound by memory.  A row is held in registers by a team of LANES threads, CHUNKS times eight elements each, and read
 // once: the sum of squares (forward) or of g * xhat (backward) needs the whole row before the first output can be
-// formed.  Teams of up to 64 lanes meet without a barrier.
+// formed.  CHUNKS is as many as the row takes, so that only the last may end inside the row: the others are read without a look at where it
+// ends.  Teams of up to 64 lanes meet without a barrier.
 #pragma once
 #include "ef_rows.h"
 
@@ -34,19 +35,17 @@ __global__ __launch_bounds__(norm_threads(LANES)) void k_norm_forward(NormForwar
     float v[CHUNKS][8];
     {
         Eight<T> e[CHUNKS];
-#pragma unroll
-        for (int c = 0; c < CHUNKS; ++c) {
-            const int64_t i = (c * LANES + lane) * 8;
-            load_some(e[c], x + i, a.n - i, 0u);
-        }
+        times<CHUNKS>([&](auto c) {
+            const int64_t i = (c.value * LANES + lane) * 8;
+            load_piece<c.value == CHUNKS - 1>(e[c.value], x + i, a.n - i);
+        });
         if (a.residual) {
             const T *r = static_cast<const T *>(a.residual) + row * a.residual_stride;
             Eight<T> f[CHUNKS];
-#pragma unroll
-            for (int c = 0; c < CHUNKS; ++c) {
-                const int64_t i = (c * LANES + lane) * 8;
-                load_some(f[c], r + i, a.n - i, 0u);
-            }
+            times<CHUNKS>([&](auto c) {
+                const int64_t i = (c.value * LANES + lane) * 8;
+                load_piece<c.value == CHUNKS - 1>(f[c.value], r + i, a.n - i);
+            });
 #pragma unroll
             for (int c = 0; c < CHUNKS; ++c)
 #pragma unroll
@@ -68,37 +67,32 @@ __global__ __launch_bounds__(norm_threads(LANES)) void k_norm_forward(NormForwar
     if (a.rstd && lane == 0) a.rstd[row] = rstd;
     if (a.h) {
         T *h = static_cast<T *>(a.h) + row * a.h_stride;
-#pragma unroll
-        for (int c = 0; c < CHUNKS; ++c) {
-            const int64_t i = (c * LANES + lane) * 8;
+        times<CHUNKS>([&](auto c) {
+            const int64_t i = (c.value * LANES + lane) * 8;
             Eight<T> e;
-            e.round(v[c]);
-            store_some(e, h + i, a.n - i);
-        }
+            e.round(v[c.value]);
+            store_piece<c.value == CHUNKS - 1>(e, h + i, a.n - i);
+        });
     }
 #pragma unroll
     for (int c = 0; c < CHUNKS; ++c)
 #pragma unroll
         for (int k = 0; k < 8; ++k) v[c][k] *= rstd;
-    if (a.act.codes) {
-#pragma unroll
-        for (int c = 0; c < CHUNKS; ++c) a.act.put(row, (c * LANES + lane) * 8, a.n, v[c]);
-    }
+    if (a.act.codes) times<CHUNKS>([&](auto c) { a.act.template put<c.value == CHUNKS - 1>(row, (c.value * LANES + lane) * 8, a.n, v[c.value]); });
     if (a.y) {
         T *y = static_cast<T *>(a.y) + row * a.y_stride;
-#pragma unroll
-        for (int c = 0; c < CHUNKS; ++c) {
-            const int64_t i = (c * LANES + lane) * 8;
+        times<CHUNKS>([&](auto c) {
+            const int64_t i = (c.value * LANES + lane) * 8;
             if (a.weight) {
                 Eight<float> w;
-                load_some(w, a.weight + i, a.n - i, 0u);
+                load_piece<c.value == CHUNKS - 1>(w, a.weight + i, a.n - i);
 #pragma unroll
-                for (int k = 0; k < 8; ++k) v[c][k] *= w[k];
+                for (int k = 0; k < 8; ++k) v[c.value][k] *= w[k];
             }
             Eight<T> e;
-            e.round(v[c]);
-            store_some(e, y + i, a.n - i);
-        }
+            e.round(v[c.value]);
+            store_piece<c.value == CHUNKS - 1>(e, y + i, a.n - i);
+        });
     }
 }
 
@@ -113,43 +107,41 @@ struct NormBackward {
     float *parts;               // [workgroups][n] sums of dy * xhat over each workgroup's rows, or NULL
 };
 
-// A team takes rows team, team + teams, ... and keeps its sums of dy * xhat in registers; a workgroup's teams add theirs up in shared
-// memory, one after the other, so that the order is fixed.
+// A team takes rows team, team + teams, ... and keeps its sums of dy * xhat in registers; a workgroup adds its teams' up through shared memory, in their
+// order.
 template <class T, int LANES, int CHUNKS>
 __global__ __launch_bounds__(norm_threads(LANES)) void k_norm_backward(NormBackward a)
 {
     constexpr int TEAMS = norm_threads(LANES) / LANES;
     __shared__ float sums[2][LANES > 64 ? LANES / 64 : 1];
-    __shared__ float joined[TEAMS > 1 ? LANES * CHUNKS * 8 : 1];
+    __shared__ float joined[TEAMS > 1 ? TEAMS : 1][TEAMS > 1 ? LANES * CHUNKS * 8 : 1];
     const int lane = threadIdx.x % LANES, team = threadIdx.x / LANES;
     float dw[CHUNKS][8], w[CHUNKS][8];
-#pragma unroll
-    for (int c = 0; c < CHUNKS; ++c) {
-        const int64_t i = (c * LANES + lane) * 8;
+    times<CHUNKS>([&](auto c) {
+        const int64_t i = (c.value * LANES + lane) * 8;
         Eight<float> e;
         if (a.weight)
-            load_some(e, a.weight + i, a.n - i, 0u);
+            load_piece<c.value == CHUNKS - 1>(e, a.weight + i, a.n - i);
         else
             e.fill(0x3f800000u);
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
-            w[c][k] = e[k];
-            dw[c][k] = 0.0f;
+            w[c.value][k] = e[k];
+            dw[c.value][k] = 0.0f;
         }
-    }
+    });
     const float per = 1.0f / (float)a.n;
     int turn = 0;
     for (int64_t row = (int64_t)blockIdx.x * TEAMS + team; row < a.rows; row += (int64_t)gridDim.x * TEAMS) {
         const T *dy = static_cast<const T *>(a.dy) + row * a.dy_stride;
         Eight<T> e[CHUNKS], f[CHUNKS];
         float x[CHUNKS][8];
-#pragma unroll
-        for (int c = 0; c < CHUNKS; ++c) {
-            const int64_t i = (c * LANES + lane) * 8;
-            load_some(e[c], dy + i, a.n - i, 0u);
-            if (a.dh) load_some(f[c], static_cast<const T *>(a.dh) + row * a.dh_stride + i, a.n - i, 0u);
-            a.act.get(row, i, x[c]);
-        }
+        times<CHUNKS>([&](auto c) {
+            const int64_t i = (c.value * LANES + lane) * 8;
+            load_piece<c.value == CHUNKS - 1>(e[c.value], dy + i, a.n - i);
+            if (a.dh) load_piece<c.value == CHUNKS - 1>(f[c.value], static_cast<const T *>(a.dh) + row * a.dh_stride + i, a.n - i);
+            a.act.template get<c.value == CHUNKS - 1>(row, i, x[c.value]);
+        });
         const float rstd = a.rstd[row];
         float s = 0.0f;
 #pragma unroll
@@ -163,47 +155,41 @@ __global__ __launch_bounds__(norm_threads(LANES)) void k_norm_backward(NormBackw
         s = over_row<Add, LANES>(s, sums[turn & 1]) * per;
         ++turn;
         T *dx = static_cast<T *>(a.dx) + row * a.dx_stride;
-#pragma unroll
-        for (int c = 0; c < CHUNKS; ++c) {
-            const int64_t i = (c * LANES + lane) * 8;
+        times<CHUNKS>([&](auto c) {
+            const int64_t i = (c.value * LANES + lane) * 8;
             float v[8];
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
-                v[k] = rstd * __builtin_fmaf(-s, x[c][k], e[c][k] * w[c][k]);
-                if (a.dh) v[k] += f[c][k];
+                v[k] = rstd * __builtin_fmaf(-s, x[c.value][k], e[c.value][k] * w[c.value][k]);
+                if (a.dh) v[k] += f[c.value][k];
             }
             Eight<T> o;
             o.round(v);
-            store_some(o, dx + i, a.n - i);
-        }
+            store_piece<c.value == CHUNKS - 1>(o, dx + i, a.n - i);
+        });
     }
     if (!a.parts) return;
     float *part = a.parts + (int64_t)blockIdx.x * a.n;
     if constexpr (TEAMS > 1) {
-        for (int t = 0; t < TEAMS; ++t) {
-            if (t == team) {
 #pragma unroll
-                for (int c = 0; c < CHUNKS; ++c)
+        for (int c = 0; c < CHUNKS; ++c)
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) {
-                        float *j = &joined[(c * 8 + k) * LANES + lane];
-                        *j = t ? *j + dw[c][k] : dw[c][k];
-                    }
-            }
-            __syncthreads();
-        }
-        for (int i = threadIdx.x; i < LANES * CHUNKS * 8; i += blockDim.x) {
-            const int l = i / 8 % LANES, c = i / 8 / LANES, k = i % 8;
-            if (i < a.n) part[i] = joined[(c * 8 + k) * LANES + l];
+            for (int k = 0; k < 8; ++k) joined[team][(c * 8 + k) * LANES + lane] = dw[c][k];
+        __syncthreads();
+        for (int i = threadIdx.x; i < a.n; i += blockDim.x) {
+            const int at = (i / 8 / LANES * 8 + i % 8) * LANES + i / 8 % LANES;
+            float s = joined[0][at];
+#pragma unroll
+            for (int t = 1; t < TEAMS; ++t) s += joined[t][at];
+            part[i] = s;
         }
     } else {
-#pragma unroll
-        for (int c = 0; c < CHUNKS; ++c) {
-            const int64_t i = (c * LANES + lane) * 8;
+        times<CHUNKS>([&](auto c) {
+            const int64_t i = (c.value * LANES + lane) * 8;
             Eight<float> e;
-            e.round(dw[c]);
-            store_some(e, part + i, a.n - i);
-        }
+            e.round(dw[c.value]);
+            store_piece<c.value == CHUNKS - 1>(e, part + i, a.n - i);
+        });
     }
 }
 

@@ -7,6 +7,8 @@
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
+#include <type_traits>
+#include <utility>
 
 namespace ef {
 
@@ -134,7 +136,8 @@ __device__ __forceinline__ float from_float<float>(float v) { return v; }
 template <>
 __device__ __forceinline__ bf16_t from_float<bf16_t>(float v) { return bf16_t{__builtin_bit_cast(uint16_t, (__bf16)v)}; }
 
-// The first `left` (any number, also none or less) of eight elements at p; `other` (a bit pattern; bf16: twice) for the rest.
+// The first `left` (any number, also none or less) of eight elements at p; `other` (a bit pattern; bf16: twice) for the rest.  A row's last elements are
+// asked for one by one, all at once.
 template <class T>
 __device__ __forceinline__ void load_some(Eight<T> &e, const T *p, int64_t left, unsigned other)
 {
@@ -143,9 +146,13 @@ __device__ __forceinline__ void load_some(Eight<T> &e, const T *p, int64_t left,
     } else {
         e.fill(other);
         if (left > 0) {
+            const int n = (int)left;
+            unsigned b[7];
+#pragma unroll
+            for (int i = 0; i < 7; ++i) b[i] = element_bits(p + min(i, n - 1));
 #pragma unroll
             for (int i = 0; i < 7; ++i)
-                if (i < left) e.set(i, element_bits(p + i));
+                e.set(i, i < n ? b[i] : sizeof(T) == 2 ? other & 0xffffu : other);
         }
     }
 }
@@ -160,6 +167,30 @@ __device__ __forceinline__ void store_some(const Eight<T> &e, T *p, int64_t left
             if (i < left) put_element(p + i, e, i);
     }
 }
+
+// The same where LAST is set; else all eight are there.
+template <bool LAST, class T>
+__device__ __forceinline__ void load_piece(Eight<T> &e, const T *p, int64_t left)
+{
+    if constexpr (LAST)
+        load_some(e, p, left, 0u);
+    else
+        e.load(p);
+}
+template <bool LAST, class T>
+__device__ __forceinline__ void store_piece(const Eight<T> &e, T *p, int64_t left)
+{
+    if constexpr (LAST)
+        store_some(e, p, left);
+    else
+        e.store(p);
+}
+
+template <class F, int... I>
+__device__ __forceinline__ void times(F f, std::integer_sequence<int, I...>) { (f(std::integral_constant<int, I>()), ...); }
+// f(0), f(1), ... f(N - 1), the index known to the compiler
+template <int N, class F>
+__device__ __forceinline__ void times(F f) { times(f, std::make_integer_sequence<int, N>()); }
 
 // ------------------------------------------------------------------------------- sums over a row's lanes ---
 
@@ -281,13 +312,15 @@ struct ActRef {
     int64_t groups;             // scales a row; a row of codes takes 32 times as many bytes
     __device__ __forceinline__ uint8_t *code_at(int64_t row, int64_t i) const { return codes + row * groups * GROUP + i; }
     __device__ __forceinline__ uint8_t *scale_at(int64_t row, int64_t i) const { return scales + row * groups + i / GROUP; }
-    // Eight values of a group, from element i (a multiple of 8) of a row of n on; the four lanes of a group call it together.
+    // Eight values of a group, from element i (a multiple of 8) of a row of n on; the four lanes of a group call it together.  Without LAST they
+    // all lie in the row.
+    template <bool LAST = true>
     __device__ __forceinline__ void put(int64_t row, int64_t i, int64_t n, const float *v) const
     {
         const unsigned byte = group_scale(v);
-        if (i >= groups * GROUP) return;
+        if (LAST && i >= groups * GROUP) return;
         u32x2 c = codes_of(v, byte);
-        if (byte == SCALE_NAN && i + 8 > n) {       // the padding stays 0
+        if (LAST && byte == SCALE_NAN && i + 8 > n) {       // the padding stays 0
             const int left = (int)max((int64_t)0, n - i);
             const unsigned long long keep = left == 0 ? 0 : ~0ull >> (64 - 8 * left);
             c.x &= (unsigned)keep;
@@ -296,9 +329,10 @@ struct ActRef {
         *reinterpret_cast<u32x2 *>(code_at(row, i)) = c;
         if (i % GROUP == 0) *scale_at(row, i) = (uint8_t)byte;
     }
+    template <bool LAST = true>
     __device__ __forceinline__ void get(int64_t row, int64_t i, float *v) const
     {
-        if (i >= groups * GROUP) {
+        if (LAST && i >= groups * GROUP) {
 #pragma unroll
             for (int k = 0; k < 8; ++k) v[k] = 0.0f;
             return;

@@ -13,7 +13,7 @@ pytestmark = pytest.mark.gpu
 EPS = 1e-6
 UNIT = oracle.EPS
 # every team: 16 lanes, a wavefront with 1, 2, 4 pieces, 256 threads with 2 and 4, 512
-WIDTHS = [1, 5, 31, 128, 129, 515, 1024, 1031, 2051, 4099, 8200, 16384]
+WIDTHS = [1, 5, 31, 128, 129, 515, 1024, 1031, 2051, 4099, 8200, 16384] + [512, 1540, 2044, 4096, 6145, 12289, 12287]
 
 
 def half_unit(dtype):
