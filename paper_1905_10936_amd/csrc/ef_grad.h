@@ -240,32 +240,32 @@ __device__ __forceinline__ int grad_lane_offset(int lane, int pitch)
     return ((block >> 1) * 8 + i / 4) * pitch + ((block & 1) * 16 + i % 4 * 4) * 2;
 }
 
-// What follows product m of region r of a 256 x 256 tile's step (sixteen products on one set of fragments): the pieces from piece[16 r + m] on up to the
-// next entry, and the halves reads[m] .. reads[m + 1] of the next region's fragments, all on their way twelve products after the region's first.
-template <int REGIONS, int PIECES>
+// What follows product m of region r of a step (a region: the products on one set of fragments): the pieces from piece[PRODUCTS r + m] on up to the next
+// entry, and the halves reads[m] .. reads[m + 1] of the next region's fragments, all on their way when three quarters of the products are.
+template <int REGIONS, int PRODUCTS, int HALVES, int PIECES>
 struct GradSchedule {
-    int piece[(REGIONS - 1) * 16 + 17] = {}, reads[17] = {};
+    int piece[REGIONS * PRODUCTS + 1] = {}, reads[PRODUCTS + 1] = {};
     constexpr GradSchedule()
     {
-        constexpr int SLOTS = (REGIONS - 1) * 16;
-        for (int k = 0; k < SLOTS + 17; ++k) piece[k] = k < SLOTS ? k * PIECES / SLOTS : PIECES;
-        int sum = 0;
-        for (int m = 0; m < 17; ++m) {
-            reads[m] = sum < 16 ? sum : 16;
-            sum += m % 4 == 0 ? 2 : 1;
-        }
+        constexpr int SLOTS = (REGIONS - 1) * PRODUCTS, EARLY = PRODUCTS * 3 / 4;
+        for (int k = 0; k <= REGIONS * PRODUCTS; ++k) piece[k] = k < SLOTS ? k * PIECES / SLOTS : PIECES;
+        for (int m = 0; m <= PRODUCTS; ++m) reads[m] = m < EARLY ? (m * HALVES + EARLY - 1) / EARLY : HALVES;
     }
 };
 
 // A step is REGIONS sets of SIDE x SIDE products a wavefront.  With SIDE = 4 there is one wavefront to a SIMD: what it does besides products has to
-// hide behind them, about four instructions of 4 to 6 cycles to a product's 32 (measured: one more costs its own time).  So everything is
-// given its place (GradSchedule): fragments are read a region ahead, words of the next step go to LDS piece by piece, and the words of the one behind
-// it are asked for as the registers get free; one barrier a step.  Smaller tiles have several workgroups on a CU that hide one another's waits.
+// hide behind them, about four instructions of 4 to 6 cycles to a product's 32 (measured: one more costs its own time).  So with SIDE = 4 and 2
+// everything is given its place (GradSchedule): fragments are read a region ahead, words of the next step go to LDS piece by piece, and words of a later
+// step are asked for as the registers get free; one barrier a step.  SIDE = 4 runs at 1.37 PFLOP/s over 16384 tokens of 4096 x 4096, what a
+// library's bf16 product of 16384 reaches here, the clock being the power's; SIDE = 2 has 110 instructions beside 16 products and is bound by issuing
+// them.  Tiles of 64 have several workgroups on a CU that hide one another's waits.
 template <class T, int SIDE>
 __global__ __launch_bounds__(GRAD_THREADS, SIDE == 4 ? 1 : 2) void k_weight_grad(GradArgs a)
 {
     using Stage = GradStage<T, SIDE>;
     constexpr int TOKENS = Stage::TOKENS, PARTS = Stage::PARTS, TILE = Stage::TILE, PITCH = Stage::PITCH, REGIONS = TOKENS / 16 * PARTS;
+    constexpr int PRODUCTS = SIDE * SIDE, HALVES = 4 * SIDE;
+    constexpr bool PLANNED = SIDE >= 2;
     __shared__ __align__(16) char buffers[2][GRAD_ROWS * PITCH];
     // Workgroups go to the eight XCDs in turn: each XCD takes a run of neighbouring tiles, which share rows of dz in its L2.
     const auto in_runs = [](int id, int all) { return id % 8 * (all / 8) + min(id % 8, all % 8) + id / 8; };
@@ -324,50 +324,71 @@ __global__ __launch_bounds__(GRAD_THREADS, SIDE == 4 ? 1 : 2) void k_weight_grad
     };
     auto put = [&](int d, char *buffer) { times<Stage::PIECES>([&](auto q) { stage.template piece<q.value, false>(a, d, buffer); }); };
     if (first < last) {
-#pragma unroll
-        for (int d = 0; d < Stage::DEPTH; ++d) fetch(first + d, d);
+        fetch(first, 0);
         put(0, now);
-        if constexpr (SIDE == 4) {
+        // the sets of words then hold the steps behind it, the same words again where there is no such step
+        if constexpr (PLANNED) {
             if (first + 1 < safe) {
-                stage.load(a, 0);
-                if (first + 2 < safe) stage.next(a);
+#pragma unroll
+                for (int d = 1; d <= Stage::DEPTH; ++d) {
+                    stage.load(a, d % Stage::DEPTH);
+                    if (first + d + 1 < safe) stage.next(a);
+                }
             }
+        } else {
+#pragma unroll
+            for (int d = 1; d < Stage::DEPTH; ++d) fetch(first + d, d);
         }
     }
     __syncthreads();
-    if constexpr (SIDE == 4) {
+    if constexpr (PLANNED) {
         if (step + 1 < safe) {
 #pragma unroll
-            for (int h = 0; h < 16; ++h) fragment(now, 0, h);
+            for (int h = 0; h < HALVES; ++h) fragment(now, 0, h);
             // Behind the products of all regions but a step's last, pieces of the next step go to LDS and the next region's fragments are read.  The last
             // region begins with the barrier and reads the next step's first fragments.
-            for (; step + 1 < safe; ++step) {
-                times<REGIONS * 16>([&](auto slot) {
-                    constexpr int r = slot.value / 16, m = slot.value % 16;
-                    constexpr GradSchedule<REGIONS, Stage::PIECES> PLAN;
-                    if constexpr (slot.value == REGIONS * 16 - 16) __syncthreads();
-                    product(r, m / 4, m % 4);
+            auto planned = [&](auto d) {
+                times<REGIONS * PRODUCTS>([&](auto slot) {
+                    constexpr int r = slot.value / PRODUCTS, m = slot.value % PRODUCTS, set = (d.value + 1) % Stage::DEPTH;
+                    constexpr GradSchedule<REGIONS, PRODUCTS, HALVES, Stage::PIECES> PLAN;
+                    if constexpr (slot.value == (REGIONS - 1) * PRODUCTS) __syncthreads();
+                    product(r, m / SIDE, m % SIDE);
                     times<PLAN.reads[m + 1] - PLAN.reads[m]>(
                         [&](auto h) { fragment(r < REGIONS - 1 ? now : next, (r + 1) % REGIONS, PLAN.reads[m] + h.value); });
                     times<PLAN.piece[slot.value + 1] - PLAN.piece[slot.value]>(
-                        [&](auto q) { stage.template piece<PLAN.piece[slot.value] + q.value, true>(a, 0, next); });
+                        [&](auto q) { stage.template piece<PLAN.piece[slot.value] + q.value, true>(a, set, next); });
                     __builtin_amdgcn_sched_barrier(0);
                 });
-                if (step + 3 < safe) stage.next(a);     // else the same words again, which nobody uses
+                if (step + Stage::DEPTH + 2 < safe) stage.next(a);
                 turn();
-            }
+                ++step;
+            };
+            // whole turns of the sets without a look at the end, then the rest
+            while (step + Stage::DEPTH < safe) times<Stage::DEPTH>(planned);
+            times<Stage::DEPTH - 1>([&](auto d) {
+                if (step + 1 < safe) planned(d);
+            });
         }
     }
     auto products = [&] {
 #pragma unroll
         for (int r = 0; r < REGIONS; ++r) {
 #pragma unroll
-            for (int h = 0; h < 4 * SIDE; ++h) fragment(now, r, h);
+            for (int h = 0; h < HALVES; ++h) fragment(now, r, h);
 #pragma unroll
-            for (int m = 0; m < SIDE * SIDE; ++m) product(r, m / SIDE, m % SIDE);
+            for (int m = 0; m < PRODUCTS; ++m) product(r, m / SIDE, m % SIDE);
         }
     };
-    if constexpr (SIDE < 4) {
+    if constexpr (PLANNED) {
+        // what is left: the step in LDS, and those that load() may not take
+        for (; step < last; ++step) {
+            if (step + 1 < last) stage.load_guarded(a, 0, (step + 1) * TOKENS, o0, n0);
+            products();
+            if (step + 1 < last) put(0, next);
+            __syncthreads();
+            turn();
+        }
+    } else {
         // without a branch: behind one, a wait for a load would be a wait for all behind it too
         for (; step + 2 * Stage::DEPTH <= safe; step += Stage::DEPTH) {
             times<Stage::DEPTH>([&](auto d) {
@@ -379,16 +400,16 @@ __global__ __launch_bounds__(GRAD_THREADS, SIDE == 4 ? 1 : 2) void k_weight_grad
                 turn();
             });
         }
-    }
-    for (; step < last; step += Stage::DEPTH) {
-        times<Stage::DEPTH>([&](auto d) {
-            if (step + d.value >= last) return;
-            fetch(step + d.value + Stage::DEPTH, d.value);
-            products();
-            if (step + d.value + 1 < last) put((d.value + 1) % Stage::DEPTH, next);
-            __syncthreads();
-            turn();
-        });
+        for (; step < last; step += Stage::DEPTH) {
+            times<Stage::DEPTH>([&](auto d) {
+                if (step + d.value >= last) return;
+                fetch(step + d.value + Stage::DEPTH, d.value);
+                products();
+                if (step + d.value + 1 < last) put((d.value + 1) % Stage::DEPTH, next);
+                __syncthreads();
+                turn();
+            });
+        }
     }
 
     // An accumulator's lane holds channel lane % 32 of x's side and four runs of four of dz's.

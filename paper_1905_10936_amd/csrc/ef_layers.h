@@ -200,13 +200,13 @@ struct GradCut {
 // The choice is the least of a sum of what was measured: a step of a tile of 256, 128 or 64 channels takes `alone` us with few workgroups on the GPU and
 // `loaded` us with as many as it holds (`most` on a CU; more slow the others down with the square of their share), a launch and a workgroup's
 // beginning and end `base`, and joining parts 4 us and 0.3 for each MB of them.  Large tiles win where there are many (4096 x 4096, 4096
-// tokens, bf16: 113, 171 and 286 us), small ones where there are few tokens (1024 x 1024, 1024 tokens: 33, 16 and 9 us), parts where there are
+// tokens, bf16: 116, 140 and 276 us), small ones where there are few tokens (1024 x 1024, 1024 tokens: 34, 14 and 9 us), parts where there are
 // many (200 x 200, 8000 tokens, tiles of 64: 42 us in one part, 12 in 8 to 16).
 GradCut grad_cut(int type, int64_t steps, int64_t out, int64_t n)
 {
     struct Side { int side, most; double alone, loaded, base; };
-    static constexpr Side SIDES[2][3] = {{{4, 1, 1.7, 2.3, 15.0}, {2, 2, 0.75, 1.55, 6.0}, {1, 3, 0.44, 0.82, 5.5}},         // EF_TYPE_FP32
-                                         {{4, 1, 1.14, 1.5, 15.0}, {2, 2, 0.64, 1.25, 6.0}, {1, 2, 0.3, 0.55, 5.5}}};
+    static constexpr Side SIDES[2][3] = {{{4, 1, 1.7, 2.3, 15.0}, {2, 2, 0.7, 1.43, 6.0}, {1, 3, 0.44, 0.82, 5.5}},         // EF_TYPE_FP32
+                                         {{4, 1, 1.14, 1.5, 15.0}, {2, 2, 0.52, 1.02, 6.0}, {1, 2, 0.3, 0.55, 5.5}}};
     GradCut best{};
     double least = 0.0;
     for (const Side &c : SIDES[type == EF_TYPE_BF16]) {
