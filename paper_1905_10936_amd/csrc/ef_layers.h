@@ -199,14 +199,14 @@ struct GradCut {
 
 // The choice is the least of a sum of what was measured: a step of a tile of 256, 128 or 64 channels takes `alone` us with few workgroups on the GPU and
 // `loaded` us with as many as it holds (`most` on a CU; more slow the others down with the square of their share), a launch and a workgroup's
-// beginning and end `base`, and joining parts 4 us and 0.3 for each MB of them.  Large tiles win where there are many (4096 x 4096, 4096
+// beginning and end `base`, and joining parts 4 us and their bytes at 4.5 TB/s.  Large tiles win where there are many (4096 x 4096, 4096
 // tokens, bf16: 116, 140 and 276 us), small ones where there are few tokens (1024 x 1024, 1024 tokens: 34, 14 and 9 us), parts where there are
 // many (200 x 200, 8000 tokens, tiles of 64: 42 us in one part, 12 in 8 to 16).
 GradCut grad_cut(int type, int64_t steps, int64_t out, int64_t n)
 {
     struct Side { int side, most; double alone, loaded, base; };
     static constexpr Side SIDES[2][3] = {{{4, 1, 1.7, 2.3, 15.0}, {2, 2, 0.7, 1.43, 6.0}, {1, 3, 0.44, 0.82, 5.5}},         // EF_TYPE_FP32
-                                         {{4, 1, 1.14, 1.5, 15.0}, {2, 2, 0.52, 1.02, 6.0}, {1, 2, 0.3, 0.55, 5.5}}};
+                                         {{4, 1, 1.14, 1.5, 15.0}, {2, 2, 0.52, 1.08, 6.0}, {1, 2, 0.3, 0.55, 5.5}}};
     GradCut best{};
     double least = 0.0;
     for (const Side &c : SIDES[type == EF_TYPE_BF16]) {
@@ -220,7 +220,7 @@ GradCut grad_cut(int type, int64_t steps, int64_t out, int64_t n)
             const int64_t part = cut * splits * tile * tile;
             if (splits > 1 && (cut == 0 || part > PART_FLOATS)) break;
             const double cost = c.base + took(whole, steps) + took(cut * splits, ceil_div(steps, splits)) +
-                                (splits > 1 ? 4.0 + 0.3 * (double)part * 4.0 / 1e6 : 0.0);
+                                (splits > 1 ? 4.0 + (double)(part + part / splits) * 4.0 / 4.5e6 : 0.0);
             if (best.side == 0 || cost < least) {
                 best = GradCut{c.side, tiles_n, tiles, splits > 1 ? whole : tiles, (int)splits};
                 least = cost;
