@@ -60,11 +60,12 @@ struct GradStage {
     static constexpr int X_WORDS = TILE / 16, X_ROWS = GRAD_THREADS / X_WORDS < TOKENS ? GRAD_THREADS / X_WORDS : TOKENS, X = TOKENS / X_ROWS;
     u32x4 z[DEPTH][Z], x[DEPTH][X];
     unsigned s[DEPTH][X];
-    // Where the step to load next begins, the same for the whole workgroup, and this thread's bytes from there.  In global memory: a load that
-    // might be LDS's would have every LDS read waited for.
+    // Where the step to load next begins, the same for the whole workgroup, and the bytes from there of each of this thread's words: a load adds the two
+    // itself, and nothing but the three bases changes from step to step.  In global memory: a load that might be LDS's would have every LDS
+    // read waited for.
     const EF_GLOBAL char *z_base;
     const EF_GLOBAL uint8_t *x_base, *s_base;
-    unsigned z_off, x_off, s_off;
+    unsigned z_off[Z], x_off[X], s_off[X];
 
     // the thread's place in a step's words of dz and of codes (threads beyond X_ROWS rows of codes do what others do)
     static __device__ __forceinline__ int z_row() { return threadIdx.x / Z_WORDS; }
@@ -79,20 +80,25 @@ struct GradStage {
         x_base = (const EF_GLOBAL uint8_t *)a.act.code_at(token0, 0);
         s_base = (const EF_GLOBAL uint8_t *)a.act.scale_at(token0, 0);
         // channels past the ends are read from the first ones
-        z_off = (unsigned)((z_row() * a.dz_stride + (o < a.out ? o : 0)) * (int64_t)sizeof(T));
-        x_off = (unsigned)(x_row() * a.act.groups * GROUP + (i < a.act.groups * GROUP ? i : 0));
-        s_off = (unsigned)(x_row() * a.act.groups + (i < a.act.groups * GROUP ? i / GROUP : 0));
+#pragma unroll
+        for (int k = 0; k < Z; ++k) z_off[k] = (unsigned)(((z_row() + k * Z_ROWS) * a.dz_stride + (o < a.out ? o : 0)) * (int64_t)sizeof(T));
+#pragma unroll
+        for (int k = 0; k < X; ++k) {
+            x_off[k] = (unsigned)((x_row() + k * X_ROWS) * a.act.groups * GROUP + (i < a.act.groups * GROUP ? i : 0));
+            s_off[k] = (unsigned)((x_row() + k * X_ROWS) * a.act.groups + (i < a.act.groups * GROUP ? i / GROUP : 0));
+        }
     }
     // The first step that load() may not take: a token's last word may reach Z_ELEMS - 1 elements past its row, and the offsets have to fit 32 bits.
     static __device__ __forceinline__ int64_t unsafe(const GradArgs &a, int64_t o0)
     {
-        if (a.dz_stride > (int64_t)1 << 26) return 0;
+        if (a.dz_stride > (int64_t)1 << 24) return 0;
         const int64_t spare = o0 + TILE <= a.out ? 0 : (Z_ELEMS - 1 + a.dz_stride - 1) / a.dz_stride;
         return max((int64_t)0, a.rows - spare) / TOKENS;
     }
     __device__ __forceinline__ void load_z(const GradArgs &a, int d, int k)
     {
-        const EF_GLOBAL char *p = z_base + (int64_t)k * Z_ROWS * a.dz_stride * (int64_t)sizeof(T) + here(z_off);
+        stay(z_off[k]);
+        const EF_GLOBAL char *p = z_base + z_off[k];
         if constexpr (sizeof(T) == 2)
             z[d][k] = *(const EF_GLOBAL u32x4_any *)p;
         else
@@ -100,8 +106,10 @@ struct GradStage {
     }
     __device__ __forceinline__ void load_x(const GradArgs &a, int d, int k)
     {
-        x[d][k] = *(const EF_GLOBAL u32x4 *)(x_base + k * X_ROWS * a.act.groups * GROUP + here(x_off));
-        s[d][k] = *(s_base + k * X_ROWS * a.act.groups + here(s_off));
+        stay(x_off[k]);
+        stay(s_off[k]);
+        x[d][k] = *(const EF_GLOBAL u32x4 *)(x_base + x_off[k]);
+        s[d][k] = *(s_base + s_off[k]);
     }
     __device__ __forceinline__ void load(const GradArgs &a, int d)
     {

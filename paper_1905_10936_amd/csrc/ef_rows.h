@@ -25,10 +25,11 @@ typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
-// An offset that is 32 bits wide where it is used: an access then adds it to a scalar base itself.
+// Keeps an offset 32 bits wide up to where it is used: an access then adds it to a scalar base itself.
+__device__ __forceinline__ void stay(unsigned &off) { asm volatile("" : "+v"(off)); }
 __device__ __forceinline__ unsigned here(unsigned off)
 {
-    asm volatile("" : "+v"(off));
+    stay(off);
     return off;
 }
 
