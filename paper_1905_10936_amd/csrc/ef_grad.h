@@ -44,7 +44,7 @@ struct GradArgs {
 };
 
 // An fp32 number is the sum of three bf16 ones: its upper half, that of what is left, and the rest, each cut off, not rounded.  Of an infinity or NaN
-// nothing is left (fmaxf takes a number over NaN).
+// nothing is left (fmaxf takes a number over NaN; a NaN is one in its upper half, as arithmetic makes them).
 __device__ __forceinline__ float upper(float v) { return __uint_as_float(__float_as_uint(v) & 0xffff0000u); }
 __device__ __forceinline__ float cut_off(float v) { return copysignf(fmaxf(fabsf(v - upper(v)), 0.0f), v); }
 __device__ __forceinline__ unsigned uppers(unsigned lo, unsigned hi) { return __builtin_amdgcn_perm(hi, lo, 0x07060302u); }

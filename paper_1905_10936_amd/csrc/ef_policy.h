@@ -316,10 +316,11 @@ __global__ __launch_bounds__(SLICE_THREADS) void k_policy_slices(PolicyArgs a, S
     if (w.masked(a)) return;
     const T *l = static_cast<const T *>(a.logits) + row * a.stride;
     const RowParts part(l, vocab);
-    const int end = min(part.whole, (slice + 1) * s.length), last = slice == 0 ? part.edge(threadIdx.x, vocab) : vocab;
+    const int64_t end = min((int64_t)part.whole, (int64_t)(slice + 1) * s.length);
+    const int last = slice == 0 ? part.edge(threadIdx.x, vocab) : vocab;
     float top = last < vocab ? to_float<T>(l[last]) : -INFINITY, sum = top == -INFINITY ? 0.0f : 1.0f;
     if (top != top) sum = top;
-    for (int i = slice * s.length + (int)threadIdx.x * 8; i < end; i += SLICE_THREADS * 8) {
+    for (int64_t i = (int64_t)slice * s.length + threadIdx.x * 8; i < end; i += SLICE_THREADS * 8) {
         Eight<T> e;
         e.load(l + part.head + i);
         more_of_row(e, top, sum);
@@ -425,10 +426,11 @@ __global__ __launch_bounds__(SLICE_THREADS) void k_policy_join(PolicyArgs a, Sli
     const T *l = static_cast<const T *>(a.logits) + row * a.stride;
     T *g = static_cast<T *>(a.dlogits) + row * a.dlogits_stride;
     const RowParts part(l, vocab);
-    const int end = min(part.whole, (slice + 1) * s.length), last = slice == 0 ? part.edge(threadIdx.x, vocab) : vocab;
+    const int64_t end = min((int64_t)part.whole, (int64_t)(slice + 1) * s.length);
+    const int last = slice == 0 ? part.edge(threadIdx.x, vocab) : vocab;
     const float top = masked ? 0.0f : joined[0], c = masked ? 0.0f : joined[2], p = masked ? 0.0f : -c / joined[1];
     const int token = masked ? -1 : (int)w.token;
-    for (int i = slice * s.length + (int)threadIdx.x * 8; i < end; i += SLICE_THREADS * 8) {
+    for (int64_t i = (int64_t)slice * s.length + threadIdx.x * 8; i < end; i += SLICE_THREADS * 8) {
         float v[8] = {};
         if (!masked) {
             Eight<T> e;
