@@ -401,7 +401,7 @@ int ef_weight_grad(ef_workspace *workspace, int64_t rows, int64_t out_width, int
     a.out = out_width;
     a.n = width;
     a.dz = dz;
-    a.dz_stride = dz_stride;
+    a.dz_stride = rows > 1 ? dz_stride : out_width;      // the kernel divides by it
     a.act = act_ref(act, rows, width);
     a.scale = column_scale;
     a.accumulate = accumulate ? 1 : 0;

@@ -124,6 +124,16 @@ def test_no_rows():
         assert bool((dw == want).all())
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("stride", [0, 1, 1 << 40])
+def test_a_single_row_has_no_stride(stride, dtype):
+    dz, x = whole_numbers(1, 300, 70, dtype, 4)
+    z = torch.as_strided(dz.to(TYPES[dtype]).cuda(), (1, 300), (stride, 1))
+    dw = torch.empty(300, 70, device="cuda")
+    ef.ef_weight_grad(ef.ef_workspace_create(1), z, encoded(x), None, dw)
+    assert torch.equal(dw.cpu(), dz.T * x)
+
+
 def test_offsets_beyond_32_bits():
     """dz rows 1.2 * 2^30 elements apart."""
     out, width, stride = 300, 64, 1288490189
