@@ -117,7 +117,7 @@ struct RowParts {
     __device__ __forceinline__ int edge(int lane, int vocab) const
     {
         if (lane < 8) return lane < head ? lane : vocab;
-        return lane < 16 ? head + whole + lane - 8 : vocab;
+        return lane < 16 && lane - 8 < vocab - head - whole ? head + whole + lane - 8 : vocab;
     }
 };
 

@@ -248,6 +248,21 @@ def test_offsets_beyond_32_bits():
     assert torch.equal(logp[live.cuda()], want[0][live.cuda()])
 
 
+@pytest.mark.parametrize("shift", [0, 1, 5])
+def test_the_largest_vocabulary(shift):
+    vocab = (1 << 31) - 1
+    base = torch.zeros(vocab + 16, dtype=torch.bfloat16, device="cuda")
+    row = base[shift:shift + vocab].view(1, vocab)
+    tokens, one = torch.tensor([vocab - 1], device="cuda"), torch.ones(1, device="cuda")
+    logp, losses, loss = (torch.empty(1, device="cuda") for _ in range(3))
+    ef.ef_policy_loss(ef.ef_workspace_create(1), row, tokens, None, None, one, None, 0.2, 0.2, 0.0, logp, losses, loss, row)
+    # equal logits: every sum of exponentials is a whole number that fp32 holds or is next to
+    assert abs(float(logp) + 31 * np.log(2)) < 4e-6 and float(loss) == -1.0
+    p = torch.tensor(2.0 ** -31).bfloat16()
+    assert bool((row[0, :-1] == p.cuda()).all()) and float(row[0, -1]) == -1.0
+    assert bool((base[:shift] == 0).all()) and bool((base[shift + vocab:] == 0).all())
+
+
 def test_streams_and_graphs():
     case = Case(40, 600, torch.bfloat16, 14)
     want = case.run()
