@@ -10,11 +10,12 @@ namespace ef {
 
 constexpr int ACT_THREADS = 256;
 
-// One thread to eight elements of the padded rows, rows one after the other.
+// One thread to eight elements of the padded rows, rows one after the other, from the `first` eight on.
 template <class T>
-__global__ __launch_bounds__(ACT_THREADS) void k_act_encode(const T *x, int64_t stride, int64_t rows, int64_t n, ActRef act)
+__global__ __launch_bounds__(ACT_THREADS) void k_act_encode(const T *x, int64_t stride, int64_t rows, int64_t n, ActRef act,
+                                                             int64_t first)
 {
-    const int64_t per_row = act.groups * (GROUP / 8), at = (int64_t)blockIdx.x * ACT_THREADS + threadIdx.x;
+    const int64_t per_row = act.groups * (GROUP / 8), at = first + (int64_t)blockIdx.x * ACT_THREADS + threadIdx.x;
     const int64_t row = at / per_row, i = (at - row * per_row) * 8;
     if (row >= rows) return;            // whole groups: four lanes at a time
     Eight<T> e;
@@ -26,9 +27,10 @@ __global__ __launch_bounds__(ACT_THREADS) void k_act_encode(const T *x, int64_t 
 }
 
 template <class T>
-__global__ __launch_bounds__(ACT_THREADS) void k_act_decode(ActRef act, int64_t rows, int64_t n, T *y, int64_t stride)
+__global__ __launch_bounds__(ACT_THREADS) void k_act_decode(ActRef act, int64_t rows, int64_t n, T *y, int64_t stride,
+                                                             int64_t first)
 {
-    const int64_t per_row = act.groups * (GROUP / 8), at = (int64_t)blockIdx.x * ACT_THREADS + threadIdx.x;
+    const int64_t per_row = act.groups * (GROUP / 8), at = first + (int64_t)blockIdx.x * ACT_THREADS + threadIdx.x;
     const int64_t row = at / per_row, i = (at - row * per_row) * 8;
     if (row >= rows) return;
     float v[8];

@@ -19,6 +19,7 @@ namespace {
 constexpr int64_t PART_FLOATS = 1 << 24;        // 64 MiB of partial results
 constexpr int64_t WIDTH_MAX = 1 << 24;
 constexpr int64_t ROWS_MAX = 0x7fffffff;
+constexpr int64_t GRID_MAX = 1 << 22;           // workgroups of a launch that grows with the rows: a grid holds less than 2^32 threads
 
 bool good_type(int type) { return type == EF_TYPE_FP32 || type == EF_TYPE_BF16; }
 size_t type_size(int type) { return type == EF_TYPE_BF16 ? 2 : 4; }
@@ -85,7 +86,7 @@ int act_args(int64_t rows, int64_t width, int type, const void *m, int64_t strid
     const Matrix a{m, stride, rows, width, type_size(type)};
     if (!a.good_stride()) return EF_ERR_ARG;
     if (!aligned(m, type_size(type)) || !aligned(act, 16)) return EF_ERR_ALIGN;
-    if (ceil_div(rows * act_groups(width) * (ef::GROUP / 8), ef::ACT_THREADS) > 0x7fffffff) return EF_ERR_SIZE;      // workgroups of the grid
+    if (ceil_div(rows * act_groups(width) * (ef::GROUP / 8), ef::ACT_THREADS) > 0x7fffffff) return EF_ERR_SIZE;      // more than any memory holds
     return share(a, vector_of(act, (int64_t)ef_act_bytes(rows, width), 1)) ? EF_ERR_ARG : EF_OK;
 }
 
@@ -100,11 +101,21 @@ int act_args(int64_t rows, int64_t width, int type, const void *m, int64_t strid
         }                                                 \
     } while (0)
 
+// `groups` workgroups in launches of GRID_MAX at most; f gets each launch's grid and the number of its first workgroup.
+template <class F>
+void in_launches(int64_t groups, F f)
+{
+    for (int64_t first = 0; first < groups; first += GRID_MAX) f(dim3((unsigned)std::min(groups - first, GRID_MAX)), first);
+}
+
 template <class T, int LANES, int CHUNKS>
-void launch_norm_forward(const ef::NormForward &a, hipStream_t s)
+void launch_norm_forward(ef::NormForward a, hipStream_t s)
 {
     constexpr int threads = ef::norm_threads(LANES);
-    hipLaunchKernelGGL((ef::k_norm_forward<T, LANES, CHUNKS>), dim3((unsigned)ceil_div(a.rows, threads / LANES)), dim3(threads), 0, s, a);
+    in_launches(ceil_div(a.rows, threads / LANES), [&](dim3 grid, int64_t first) {
+        a.first = first * (threads / LANES);
+        hipLaunchKernelGGL((ef::k_norm_forward<T, LANES, CHUNKS>), grid, dim3(threads), 0, s, a);
+    });
 }
 template <class T, int LANES, int CHUNKS>
 int launch_norm_backward(ef::NormBackward &a, hipStream_t s)
@@ -264,9 +275,10 @@ int ef_act_encode(int64_t rows, int64_t width, int type, const void *x, int64_t 
     const int rc = act_args(rows, width, type, x, x_stride, act);
     if (rc || !rows) return rc;
     const ef::ActRef r = act_ref(act, rows, width);
-    const dim3 grid((unsigned)ceil_div(rows * r.groups * (ef::GROUP / 8), ef::ACT_THREADS));
-    EF_BY_TYPE(type, T, hipLaunchKernelGGL(ef::k_act_encode<T>, grid, dim3(ef::ACT_THREADS), 0, static_cast<hipStream_t>(stream),
-                                           static_cast<const T *>(x), x_stride, rows, width, r));
+    in_launches(ceil_div(rows * r.groups * (ef::GROUP / 8), ef::ACT_THREADS), [&](dim3 grid, int64_t first) {
+        EF_BY_TYPE(type, T, hipLaunchKernelGGL(ef::k_act_encode<T>, grid, dim3(ef::ACT_THREADS), 0, static_cast<hipStream_t>(stream),
+                                               static_cast<const T *>(x), x_stride, rows, width, r, first * ef::ACT_THREADS));
+    });
     EF_HIP(hipGetLastError());
     return EF_OK;
 }
@@ -276,9 +288,10 @@ int ef_act_decode(int64_t rows, int64_t width, const void *act, int type, void *
     const int rc = act_args(rows, width, type, y, y_stride, act);
     if (rc || !rows) return rc;
     const ef::ActRef r = act_ref(act, rows, width);
-    const dim3 grid((unsigned)ceil_div(rows * r.groups * (ef::GROUP / 8), ef::ACT_THREADS));
-    EF_BY_TYPE(type, T, hipLaunchKernelGGL(ef::k_act_decode<T>, grid, dim3(ef::ACT_THREADS), 0, static_cast<hipStream_t>(stream), r, rows,
-                                           width, static_cast<T *>(y), y_stride));
+    in_launches(ceil_div(rows * r.groups * (ef::GROUP / 8), ef::ACT_THREADS), [&](dim3 grid, int64_t first) {
+        EF_BY_TYPE(type, T, hipLaunchKernelGGL(ef::k_act_decode<T>, grid, dim3(ef::ACT_THREADS), 0, static_cast<hipStream_t>(stream), r, rows,
+                                               width, static_cast<T *>(y), y_stride, first * ef::ACT_THREADS));
+    });
     EF_HIP(hipGetLastError());
     return EF_OK;
 }
@@ -303,7 +316,7 @@ int ef_norm_forward(int64_t rows, int64_t width, int type, const void *x, int64_
     if (!apart(out, 4, in, 3, in_place)) return EF_ERR_ARG;
     if (!rows) return EF_OK;
     const ef::NormForward a{rows, width, x, residual, x_stride, residual_stride, weight, eps, h, y, h_stride, y_stride,
-                            act_ref(act, rows, width), rstd};
+                            act_ref(act, rows, width), rstd, 0};
     const hipStream_t s = static_cast<hipStream_t>(stream);
 #define EF_CALL(LANES, CHUNKS) launch_norm_forward<T, LANES, CHUNKS>(a, s)
     EF_BY_TYPE(type, T, EF_NORM_TEAM(width, EF_CALL));

@@ -21,6 +21,7 @@ struct NormForward {
     int64_t h_stride, y_stride;
     ActRef act;                 // codes == nullptr: none is written
     float *rstd;
+    int64_t first;              // the launch's first row
 };
 
 constexpr int norm_threads(int lanes) { return lanes < 256 ? 256 : lanes; }
@@ -31,7 +32,7 @@ __global__ __launch_bounds__(norm_threads(LANES)) void k_norm_forward(NormForwar
     constexpr int TEAMS = norm_threads(LANES) / LANES;
     __shared__ float sums[LANES > 64 ? LANES / 64 : 1];
     const int lane = threadIdx.x % LANES;
-    const int64_t row = (int64_t)blockIdx.x * TEAMS + threadIdx.x / LANES;
+    const int64_t row = a.first + (int64_t)blockIdx.x * TEAMS + threadIdx.x / LANES;
     if (row >= a.rows) return;          // whole teams; LANES > 64: never
     const T *x = static_cast<const T *>(a.x) + row * a.x_stride;
     float v[CHUNKS][8];

@@ -125,6 +125,20 @@ def test_offsets_beyond_32_bits():
     assert torch.equal(x, want)
 
 
+def test_more_groups_than_a_launch_has_threads_for():
+    rows = (1 << 30) + 37            # four threads to a group of one element
+    x = torch.full((rows, 1), 1.0, dtype=torch.bfloat16, device="cuda")
+    x[-30:, 0] = torch.arange(1, 31, device="cuda").bfloat16()
+    act = torch.zeros(ef.ef_act_bytes(rows, 1), dtype=torch.uint8, device="cuda")
+    ef.ef_act_encode(x, act)
+    y = torch.zeros_like(x)
+    ef.ef_act_decode(act, y)
+    # the numbers' distance from E4M3's, which is the same under any scale
+    want = x.clone()
+    want[-30:] = x[-30:].float().to(torch.float8_e4m3fn).bfloat16()
+    assert torch.equal(y, want)
+
+
 def test_no_rows():
     x, act = torch.empty(0, 40, device="cuda"), torch.empty(0, dtype=torch.uint8, device="cuda")
     assert ef.ef_act_bytes(0, 40) == 0

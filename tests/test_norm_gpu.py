@@ -254,6 +254,17 @@ def test_offsets_beyond_32_bits():
     assert torch.equal(close, x)
 
 
+def test_more_rows_than_a_launch_has_threads_for():
+    rows = (1 << 28) + 21            # 16 threads to a row
+    x = torch.full((rows, 1), 3.0, dtype=torch.bfloat16, device="cuda")
+    x[-20:, 0] = -torch.arange(1, 21, device="cuda").bfloat16()
+    rstd = torch.zeros(rows, device="cuda")
+    ef.ef_norm_forward(x, None, None, 0.0, None, x, None, rstd)
+    assert bool((x[:-20] == 1).all()) and bool((x[-20:] == -1).all())
+    assert bool(((rstd[:-20] * 3 - 1).abs() < 4 * UNIT).all())
+    assert bool(((rstd[-20:] * torch.arange(1, 21, device="cuda") - 1).abs() < 4 * UNIT).all())
+
+
 def test_streams_and_graphs():
     """On a stream of its own, and captured: every replay the eager result, with other work between the replays."""
     rows, n = 64, 300         # a checkpoint without padding, which no call writes
