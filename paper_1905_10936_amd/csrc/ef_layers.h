@@ -150,11 +150,23 @@ void launch_policy(const ef::PolicyArgs &a, hipStream_t s)
     hipLaunchKernelGGL((ef::k_policy<T, LANES, CHUNKS>), dim3((unsigned)groups), dim3(threads), 0, s, a);
 }
 
+// A workgroup to a row, with as many eights a thread as the row takes: one more at a time up to 8, two beyond.
+template <class T, int CHUNKS = 2>
+void policy_workgroups(const ef::PolicyArgs &a, hipStream_t s)
+{
+    if constexpr (CHUNKS > ef::policy_chunks<T>)
+        hipLaunchKernelGGL(ef::k_policy_long<T>, dim3((unsigned)a.rows), dim3(ef::LONG_THREADS), 0, s, a);
+    else if (a.vocab <= CHUNKS * 8192)
+        launch_policy<T, 1024, CHUNKS>(a, s);
+    else
+        policy_workgroups<T, CHUNKS + (CHUNKS < 8 ? 1 : 2)>(a, s);
+}
+
 template <class T>
 void policy_rows(const ef::PolicyArgs &a, hipStream_t s)
 {
     // 16 lanes up to 512 entries (a row's own arithmetic, a hundred instructions, is then four rows' at a time: 32768 rows of 259 in bf16 32 us with 64
-    // lanes, 22 with 16), a wavefront up to 2048 (no barrier), 256 threads up to 8192, 1024 beyond, with as many eights a thread as the row takes
+    // lanes, 22 with 16), a wavefront up to 2048 (no barrier), 256 threads up to 8192, 1024 beyond
     const int64_t n = a.vocab;
     if (n <= 128)
         launch_policy<T, 16, 1>(a, s);
@@ -164,18 +176,8 @@ void policy_rows(const ef::PolicyArgs &a, hipStream_t s)
         launch_policy<T, 64, 4>(a, s);
     else if (n <= 8192)
         launch_policy<T, 256, 4>(a, s);
-    else if (n > 65536)
-        hipLaunchKernelGGL(ef::k_policy_long<T>, dim3((unsigned)a.rows), dim3(ef::LONG_THREADS), 0, s, a);
     else
-        switch ((n + 8191) / 8192) {
-        case 2: launch_policy<T, 1024, 2>(a, s); break;
-        case 3: launch_policy<T, 1024, 3>(a, s); break;
-        case 4: launch_policy<T, 1024, 4>(a, s); break;
-        case 5: launch_policy<T, 1024, 5>(a, s); break;
-        case 6: launch_policy<T, 1024, 6>(a, s); break;
-        case 7: launch_policy<T, 1024, 7>(a, s); break;
-        default: launch_policy<T, 1024, 8>(a, s); break;
-        }
+        policy_workgroups<T>(a, s);
 }
 
 template <class T>
@@ -184,7 +186,7 @@ void policy_slices(const ef::PolicyArgs &a, float *parts, float *loss, hipStream
     ef::SliceRef r;
     r.joint = reinterpret_cast<float2 *>(parts);
     r.chosen = parts + 2 * ef::SLICED_ROWS * ef::SLICES_MAX;
-    r.count = (int)std::min<int64_t>(ceil_div(a.vocab, ef::SLICE), ef::SLICES_MAX);
+    r.count = (int)std::min<int64_t>(ceil_div(a.vocab, ef::SLICE), std::min<int64_t>(ef::SLICES_MAX, ceil_div(ef::SLICES_ALL, a.rows)));
     r.length = (int)(ceil_div(a.vocab, r.count * 8) * 8);
     const dim3 grid((unsigned)(a.rows * r.count));
     hipLaunchKernelGGL(ef::k_policy_slices<T>, grid, dim3(ef::SLICE_THREADS), 0, s, a, r);

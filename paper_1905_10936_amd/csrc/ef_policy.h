@@ -244,7 +244,12 @@ __device__ __forceinline__ void more_of_row(const Eight<T> &e, float &top, float
     }
 }
 
-// Rows longer than a workgroup's registers: maximum and sum kept up to date chunk by chunk, the row read again for the gradient.
+// The longest rows a workgroup has in registers: 196608 entries in bf16, 98304 in fp32, 96 registers a thread of the 128 there are.  2048 rows of 128256 in
+// bf16 take 227 us, 266 where a row is read again for its gradient; of 196000 357 and 450; of 80000 in fp32 269 and 340.
+template <class T>
+constexpr int policy_chunks = sizeof(T) == 2 ? 24 : 12;
+
+// Longer rows: maximum and sum kept up to date chunk by chunk, the row read again for the gradient.
 constexpr int LONG_THREADS = 1024;
 template <class T>
 __global__ __launch_bounds__(LONG_THREADS) void k_policy_long(PolicyArgs a)
@@ -299,7 +304,8 @@ __global__ __launch_bounds__(LONG_THREADS) void k_policy_long(PolicyArgs a)
 // Few rows of many entries: a row cut into slices, a workgroup each, in two kernels.  The first leaves every slice's maximum and sum of exponentials, and the
 // token's logit; in the second each workgroup joins its row's and writes its slice's gradient.  5 rows of 50304 in fp32: 11.8 us with a
 // workgroup to a row, 8.3 with 25; 16 rows of 200000 in bf16: 34.6 and 11.2; 16 of 9000, where a workgroup has its row in registers: 8.0 and 8.3.
-constexpr int SLICE_THREADS = 256, SLICE = 2048, SLICES_MAX = 64, SLICED_ROWS = 64, SLICED_VOCAB = 32768;
+// About SLICES_ALL workgroups at most: 64 rows of 128256 in bf16 14.5 us with 16 slices a row, 17.5 with 63.
+constexpr int SLICE_THREADS = 256, SLICE = 2048, SLICES_MAX = 64, SLICES_ALL = 1024, SLICED_ROWS = 64, SLICED_VOCAB = 32768;
 struct SliceRef {
     float2 *joint;              // [rows][SLICES_MAX] maximum, sum of 2^((l - maximum) L)
     float *chosen;              // [rows]

@@ -88,6 +88,20 @@ def test_more_rows_of_large_vocabularies(vocab, dtype):
     assert all(torch.equal(a, b) for a, b in zip(got, case.run(dlogits=lambda logits: logits)))
 
 
+@pytest.mark.parametrize("vocab,dtype", [(81921, "bf16"), (98299, "bf16"), (131073, "bf16"), (152001, "bf16"), (196601, "bf16"), (196609, "bf16"),
+                                         (81923, "fp32"), (98304, "fp32"), (98305, "fp32")])
+def test_the_longest_rows_in_registers(vocab, dtype):
+    case = Case(65, vocab, TYPES[dtype], vocab, pad=9)
+    case.weight[2], case.tokens[1] = 0.0, vocab - 10
+    got = case.run()
+    case.check(got)
+    assert all(torch.equal(a, b) for a, b in zip(got, case.run(dlogits=lambda logits: logits)))
+    logp = torch.empty(65, device="cuda")
+    ef.ef_token_logp(case.logits.cuda(), case.tokens.cuda(), logp)
+    live = case.weight != 0
+    assert torch.equal(logp[live.cuda()], got[0][live.cuda()])
+
+
 @pytest.mark.parametrize("rows", [1, 7, 33, 64])
 def test_slices(rows):
     case = Case(rows, 40001, torch.bfloat16, rows, pad=3)
