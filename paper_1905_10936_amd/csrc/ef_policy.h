@@ -145,12 +145,16 @@ __global__ __launch_bounds__(policy_threads(LANES), LANES == 1024 && sizeof(T) *
         const T *l = static_cast<const T *>(a.logits) + row * a.stride;
         const RowParts part(l, vocab);
         const int whole = part.whole, last = part.edge(lane, vocab), chunks = (whole + LANES * 8 - 1) / (LANES * 8);
+        // Of chunk c a thread has the eight from byte `from(c)` of the whole part on: formed where it is used (a number kept for each chunk costs registers:
+        // 2048 rows of 65000 in bf16 140 us, 119 this way).
+        const auto from = [&](int c) { return here(off) + c * LANES * 8 * (unsigned)sizeof(T); };
+        const unsigned whole_bytes = whole * (unsigned)sizeof(T);
         Eight<T> e[CHUNKS];
 #pragma unroll
         for (int c = 0; c < CHUNKS; ++c) {
-            const int i = (c * LANES + lane) * 8;
+            const unsigned at = from(c);
             e[c].fill(NONE);
-            if (i < whole) e[c].load_at(l + part.head + c * LANES * 8, off);
+            if (at < whole_bytes) e[c].load_at(l + part.head, at);
         }
         const float tail = last < vocab ? to_float<T>(l[last]) : -INFINITY;
         // The token's logit goes into the maximum: it is there before the row's first barrier, and the gradient may be written over the row
@@ -197,22 +201,22 @@ __global__ __launch_bounds__(policy_threads(LANES), LANES == 1024 && sizeof(T) *
         }
         T *g = static_cast<T *>(a.dlogits) + row * a.dlogits_stride;
         const float p = -f.y / sum;
+        const unsigned token_at = ((int)w.token - part.head) * (unsigned)sizeof(T);         // wraps where it lies before the whole part
 #pragma unroll
         for (int c = 0; c < CHUNKS; ++c) {
             if (c < chunks) {
-                const int i = (c * LANES + lane) * 8;
+                const unsigned to = from(c), at = token_at - to;
                 float v[8];
 #pragma unroll
                 for (int k = 0; k < 8; ++k) v[k] = x.of(e[c][k]) * p;
-                const int at = (int)w.token - part.head - i;
-                if ((unsigned)at < 8u) {
+                if (at < 8 * sizeof(T)) {
 #pragma unroll
                     for (int k = 0; k < 8; ++k)
-                        if (at == k) v[k] += f.y;
+                        if (at == k * sizeof(T)) v[k] += f.y;
                 }
                 Eight<T> o;
                 o.round(v);
-                if (i < whole) o.store_at(g + part.head + c * LANES * 8, off);
+                if (to < whole_bytes) o.store_at(g + part.head, to);
             }
             __builtin_amdgcn_sched_barrier(0);
         }
@@ -245,7 +249,7 @@ __device__ __forceinline__ void more_of_row(const Eight<T> &e, float &top, float
 }
 
 // The longest rows a workgroup has in registers: 196608 entries in bf16, 98304 in fp32, 96 registers a thread of the 128 there are.  2048 rows of 128256 in
-// bf16 take 227 us, 266 where a row is read again for its gradient; of 196000 357 and 450; of 80000 in fp32 269 and 340.
+// bf16 take 225 us, 266 where a row is read again for its gradient; of 196000 350 and 450; of 80000 in fp32 268 and 340.
 template <class T>
 constexpr int policy_chunks = sizeof(T) == 2 ? 24 : 12;
 
