@@ -121,8 +121,11 @@ template <class T, int LANES, int CHUNKS>
 int launch_norm_backward(ef::NormBackward &a, hipStream_t s)
 {
     constexpr int threads = ef::norm_threads(LANES);
-    // as many workgroups as have rows, up to two to a CU; their sums have to fit the workspace
-    const int64_t groups = std::min(std::min(ceil_div(a.rows, threads / LANES), (int64_t)512), PART_FLOATS / a.n);
+    // As many workgroups as have rows, up to two to a CU, or one where they are of 512 threads or two would leave a team no more than two rows: the workgroups'
+    // sums are written and read (bf16, one and two to a CU: 512 x 8192 15.1 and 17.4 us, 2048 x 16384 54.5 and 60.1, 4096 x 4096 32.1 and 28.6).
+    // They have to fit the workspace.
+    const int64_t turns = ceil_div(a.rows, threads / LANES), most = threads >= 512 || turns <= 1024 ? 256 : 512;
+    const int64_t groups = std::min(std::min(turns, most), PART_FLOATS / a.n);
     hipLaunchKernelGGL((ef::k_norm_backward<T, LANES, CHUNKS>), dim3((unsigned)groups), dim3(threads), 0, s, a);
     return (int)groups;
 }
