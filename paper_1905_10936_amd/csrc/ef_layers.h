@@ -339,7 +339,7 @@ int ef_workspace_create(ef_workspace **out, int64_t max_rows, void *stream)
     ef_workspace *w = new (std::nothrow) ef_workspace();
     if (!w) return EF_ERR_ARG;
     w->max_rows = max_rows;
-    const size_t rows_bytes = ((size_t)max_rows * 16 + 255) / 256 * 256;
+    const size_t rows_bytes = ((size_t)max_rows * sizeof(float) + 255) / 256 * 256;
     hipError_t e = hipGetDevice(&w->device);
     if (e == hipSuccess) e = hipMalloc(&w->base, rows_bytes + sizeof(float) * (size_t)PART_FLOATS);
     if (e != hipSuccess) {
