@@ -153,34 +153,27 @@ void launch_policy(const ef::PolicyArgs &a, hipStream_t s)
     hipLaunchKernelGGL((ef::k_policy<T, LANES, CHUNKS>), dim3((unsigned)groups), dim3(threads), 0, s, a);
 }
 
-// A workgroup to a row, with as many eights a thread as the row takes: one more at a time up to 8, two beyond.
-template <class T, int CHUNKS = 2>
-void policy_workgroups(const ef::PolicyArgs &a, hipStream_t s)
+// The first of the listed teams that holds a row; false: none does.
+template <class T, int LANES, int... CHUNKS>
+bool policy_teams(const ef::PolicyArgs &a, hipStream_t s)
 {
-    if constexpr (CHUNKS > ef::policy_chunks<T>)
-        hipLaunchKernelGGL(ef::k_policy_long<T>, dim3((unsigned)a.rows), dim3(ef::LONG_THREADS), 0, s, a);
-    else if (a.vocab <= CHUNKS * 8192)
-        launch_policy<T, 1024, CHUNKS>(a, s);
-    else
-        policy_workgroups<T, CHUNKS + (CHUNKS < 8 ? 1 : 2)>(a, s);
+    return ((a.vocab <= LANES * 8 * CHUNKS && (launch_policy<T, LANES, CHUNKS>(a, s), true)) || ...);
 }
 
+// A row's own arithmetic, a hundred instructions, is a wavefront's whatever the row's length, so short rows are four to a wavefront (32768 rows of 259 in bf16
+// 22 us, 32 with a wavefront to a row; of 600 20 and 31); it costs a workgroup three barriers besides, so a wavefront has rows of up to 4096 or 5120 (16384
+// of 2500 in bf16 41 us, 66 with 256 threads) and a thread of a workgroup many eights where its type lets it (bf16, in us: 8192 x 9000 65 with
+// 256 threads, 99 with 1024; 4096 x 18000 63 and 73; 2048 x 65000 115 with 512, 120 with 1024).  fp32 gains nothing there.
 template <class T>
 void policy_rows(const ef::PolicyArgs &a, hipStream_t s)
 {
-    // 16 lanes up to 512 entries (a row's own arithmetic, a hundred instructions, is then four rows' at a time: 32768 rows of 259 in bf16 32 us with 64
-    // lanes, 22 with 16), a wavefront up to 2048 (no barrier), 256 threads up to 8192, 1024 beyond
-    const int64_t n = a.vocab;
-    if (n <= 128)
-        launch_policy<T, 16, 1>(a, s);
-    else if (n <= 512)
-        launch_policy<T, 16, 4>(a, s);
-    else if (n <= 2048)
-        launch_policy<T, 64, 4>(a, s);
-    else if (n <= 8192)
-        launch_policy<T, 256, 4>(a, s);
+    bool done = false;
+    if constexpr (sizeof(T) == 2)
+        done = policy_teams<T, 16, 1, 4, 8>(a, s) || policy_teams<T, 64, 4, 8, 10>(a, s) || policy_teams<T, 256, 4, 8, 12>(a, s) || policy_teams<T, 1024, 4, 5>(a, s) ||
+               policy_teams<T, 512, 12, 14, 16>(a, s) || policy_teams<T, 1024, 10, 12, 14, 16, 18, 20, 22, 24>(a, s);
     else
-        policy_workgroups<T>(a, s);
+        done = policy_teams<T, 16, 1, 4, 6>(a, s) || policy_teams<T, 64, 4, 8>(a, s) || policy_teams<T, 256, 4>(a, s) || policy_teams<T, 1024, 2, 3, 4, 5, 6, 7, 8, 10, 12>(a, s);
+    if (!done) hipLaunchKernelGGL(ef::k_policy_long<T>, dim3((unsigned)a.rows), dim3(ef::LONG_THREADS), 0, s, a);
 }
 
 template <class T>

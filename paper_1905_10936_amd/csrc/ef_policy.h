@@ -248,12 +248,9 @@ __device__ __forceinline__ void more_of_row(const Eight<T> &e, float &top, float
     }
 }
 
-// The longest rows a workgroup has in registers: 196608 entries in bf16, 98304 in fp32, 96 registers a thread of the 128 there are.  2048 rows of 128256 in
-// bf16 take 225 us, 266 where a row is read again for its gradient; of 196000 350 and 450; of 80000 in fp32 268 and 340.
-template <class T>
-constexpr int policy_chunks = sizeof(T) == 2 ? 24 : 12;
-
-// Longer rows: maximum and sum kept up to date chunk by chunk, the row read again for the gradient.
+// Rows longer than a workgroup's registers (196608 entries in bf16, 98304 in fp32: 96 registers a thread of the 128 there are; 2048 rows of 128256 in bf16
+// take 225 us that way, 266 here; of 196000 350 and 450; of 80000 in fp32 268 and 340): maximum and sum kept up to date chunk by chunk, the row read again
+// for the gradient.
 constexpr int LONG_THREADS = 1024;
 template <class T>
 __global__ __launch_bounds__(LONG_THREADS) void k_policy_long(PolicyArgs a)

@@ -102,6 +102,17 @@ def test_the_longest_rows_in_registers(vocab, dtype):
     assert torch.equal(logp[live.cuda()], got[0][live.cuda()])
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("vocab", [129, 513, 767, 769, 1023, 1025, 2049, 4095, 4097, 5121, 8193, 16383, 16385, 24577, 32769, 40961, 49153, 65536])
+def test_every_team(vocab, dtype):
+    """Around the lengths where a row goes to another team."""
+    case = Case(67, vocab, TYPES[dtype], vocab, pad=2)
+    case.weight[5], case.tokens[9] = 0.0, 0
+    got = case.run()
+    case.check(got)
+    assert all(torch.equal(a, b) for a, b in zip(got, case.run(dlogits=lambda logits: logits)))
+
+
 @pytest.mark.parametrize("rows", [1, 7, 33, 64])
 def test_slices(rows):
     case = Case(rows, 40001, torch.bfloat16, rows, pad=3)
