@@ -7,7 +7,8 @@
 // reaches 5.1.
 //
 // exp(l - m) is 2^(l * L - c) with L = log2(e) rounded and c = m * L rounded, one fused operation and one exponential an element; what
-// c was rounded by is put right once a row.
+// c was rounded by is put right once a row.  That holds as long as it is little beside the exponents that count: rows whose maximum m is a large number
+// (LARGE) have it taken off first, without a rounding of its product.
 #pragma once
 #include "ef_rows.h"
 
@@ -72,19 +73,36 @@ __device__ __forceinline__ float2 row_loss(const PolicyArgs &a, const RowArgs &w
     return make_float2(w.q * f, w.q * c);
 }
 
+// A row's maximum that is larger in size: c would be rounded by more than 2^-4, and from 2^31 on by more than an exponential's range.
+constexpr float LARGE = 0x1p20f;
+
 struct Exponent {
     float factor, c;
-    // Where the largest logit is itself beyond 10^30 in size (a mask of the type's lowest value in every place), m * L would overflow, and any other
-    // logit is at least 2^76 away: 2^-20 for L, which multiplies exactly, gives 1 and 0 as e would.
+    // From LARGE on bf16 numbers are 2^12 apart and more, so that any other logit's exponential is 0 whatever the factor: 1 multiplies exactly.
+    // A row of fp32 comes here with its maximum taken off (shift_large).
     __device__ __forceinline__ explicit Exponent(float top)
     {
-        factor = fabsf(top) > 1e30f ? 0x1p-20f : LOG2E;
+        factor = fabsf(top) > LARGE ? 1.0f : LOG2E;
         c = top * factor;
     }
     __device__ __forceinline__ float of(float l) const { return __builtin_amdgcn_exp2f(__builtin_fmaf(l, factor, -c)); }
     // log of the row's sum of exponentials less `top`, from the sum of of(l)
     __device__ __forceinline__ float log_sum(float sum, float top) const { return logf(sum) - LN2 * __builtin_fmaf(top, factor, -c); }
 };
+
+// A row of fp32 whose maximum is large in size less that maximum, in place: 0 and the differences, each rounded once.
+template <int CHUNKS>
+__device__ __forceinline__ void shift_large(Eight<float> (&e)[CHUNKS], float &tail, float &chosen, float &top)
+{
+    if (!(fabsf(top) > LARGE)) return;
+#pragma unroll
+    for (int c = 0; c < CHUNKS; ++c)
+#pragma unroll
+        for (int k = 0; k < 8; ++k) e[c].set(k, __float_as_uint(e[c][k] - top));
+    tail -= top;
+    chosen -= top;
+    top = 0.0f;
+}
 
 constexpr int policy_threads(int lanes) { return lanes < 256 ? 256 : lanes; }
 
@@ -156,10 +174,10 @@ __global__ __launch_bounds__(policy_threads(LANES), LANES == 1024 && sizeof(T) *
             e[c].fill(NONE);
             if (at < whole_bytes) e[c].load_at(l + part.head, at);
         }
-        const float tail = last < vocab ? to_float<T>(l[last]) : -INFINITY;
+        float tail = last < vocab ? to_float<T>(l[last]) : -INFINITY;
         // The token's logit goes into the maximum: it is there before the row's first barrier, and the gradient may be written over the row
         // behind it.
-        const float chosen = to_float<T>(l[w.token]);
+        float chosen = to_float<T>(l[w.token]);
         float top = fmaxf(chosen, tail);
 #pragma unroll
         for (int c = 0; c < CHUNKS; ++c) {
@@ -170,6 +188,7 @@ __global__ __launch_bounds__(policy_threads(LANES), LANES == 1024 && sizeof(T) *
             __builtin_amdgcn_sched_barrier(0);
         }
         top = over_row<Max, LANES>(top, tops);
+        if constexpr (sizeof(T) == 4) shift_large(e, tail, chosen, top);
         const Exponent x(top);
         float sum = x.of(tail);
 #pragma unroll
