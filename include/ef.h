@@ -391,7 +391,8 @@ int ef_compressor_quality_static(const ef_plan *plan, int n_vectors, const float
  * by side in one buffer (same stride, different columns) do not share memory.
  * Sums, means and products are accumulated in fp32 or wider in a fixed order:
  * repeated calls give the same bits.  Infinities and NaN go where the formulas
- * take them.  rows = 0 is a valid call: sums over no rows are zero.
+ * take them.  rows = 0 is a valid call: sums over no rows are zero, and the
+ * pointers whose arrays then hold nothing may be NULL.
  */
 #define EF_TYPE_FP32 0
 #define EF_TYPE_BF16 1

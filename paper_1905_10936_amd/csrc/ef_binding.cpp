@@ -98,7 +98,8 @@ public:
         return t;
     }
     const at::Tensor *floats() { return tensor(at::kFloat); }
-    // a 1-D tensor (one row) or a 2-D one of either type, its rows contiguous, on the GPU
+    // a 1-D tensor (one row) or a 2-D one of either type, its rows contiguous, on the GPU; an empty one, whose address is null like that of none at
+    // all, is left to the caller's other path
     Mat matrix()
     {
         Mat m;
@@ -114,6 +115,7 @@ public:
         m.stride = t.dim() == 1 ? m.width : t.stride(0);
         ok = m.width < 2 || t.stride(-1) == 1;
         m.p = t.data_ptr();
+        ok = ok && m.p;
         return m;
     }
     // the same or None, of another matrix's shape and type

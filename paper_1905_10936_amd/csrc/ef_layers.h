@@ -26,6 +26,10 @@ size_t type_size(int type) { return type == EF_TYPE_BF16 ? 2 : 4; }
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 int64_t act_groups(int64_t width) { return ceil_div(width, ef::GROUP); }
 
+// Is one of the pointers missing that a call on rows needs?  Without rows they point to nothing, and an empty tensor's address is null.
+template <class... P>
+bool missing(int64_t rows, const P *...p) { return rows != 0 && (!p || ...); }
+
 // A matrix argument as the checks see it; p == nullptr: not given.
 struct Matrix {
     const void *p;
@@ -81,7 +85,7 @@ int on_workspace_device(const ef_workspace *w)
 
 int act_args(int64_t rows, int64_t width, int type, const void *m, int64_t stride, const void *act)
 {
-    if (!m || !act) return EF_ERR_NULL;
+    if (missing(rows, m, act)) return EF_ERR_NULL;
     if (rows < 0 || rows > ROWS_MAX || width < 1 || width > WIDTH_MAX || !good_type(type)) return EF_ERR_ARG;
     const Matrix a{m, stride, rows, width, type_size(type)};
     if (!a.good_stride()) return EF_ERR_ARG;
@@ -191,7 +195,7 @@ void policy_slices(const ef::PolicyArgs &a, float *parts, float *loss, hipStream
 
 int policy_args(int64_t rows, int64_t vocab, int type, const void *logits, int64_t stride, const int64_t *tokens)
 {
-    if (!logits || !tokens) return EF_ERR_NULL;
+    if (missing(rows, logits, tokens)) return EF_ERR_NULL;
     if (rows < 0 || rows > ROWS_MAX || vocab < 1 || vocab > 0x7fffffff || !good_type(type)) return EF_ERR_ARG;
     const Matrix l{logits, stride, rows, vocab, type_size(type)};
     if (!l.good_stride()) return EF_ERR_ARG;
@@ -298,7 +302,7 @@ int ef_norm_forward(int64_t rows, int64_t width, int type, const void *x, int64_
                     int64_t residual_stride, const float *weight, float eps, void *h, int64_t h_stride, void *y, int64_t y_stride,
                     void *act, float *rstd, void *stream)
 {
-    if (!x || (!h && !y && !act && !rstd)) return EF_ERR_NULL;
+    if (missing(rows, x) || (rows && !h && !y && !act && !rstd)) return EF_ERR_NULL;
     if (rows < 0 || rows > ROWS_MAX || width < 1 || !good_type(type) || !(std::isfinite(eps) && eps >= 0.0f)) return EF_ERR_ARG;
     if (width > EF_NORM_MAX_WIDTH) return EF_ERR_SIZE;
     const size_t size = type_size(type);
@@ -358,7 +362,7 @@ int ef_norm_backward(ef_workspace *workspace, int64_t rows, int64_t width, int t
                      const void *act, const float *rstd, const float *weight, const void *dh, int64_t dh_stride, void *dx,
                      int64_t dx_stride, float *dweight, int accumulate, void *stream)
 {
-    if (!workspace || !dy || !act || !rstd || !dx) return EF_ERR_NULL;
+    if (!workspace || missing(rows, dy, act, rstd, dx)) return EF_ERR_NULL;
     if (rows < 0 || rows > ROWS_MAX || width < 1 || !good_type(type)) return EF_ERR_ARG;
     if (width > EF_NORM_MAX_WIDTH || rows > workspace->max_rows) return EF_ERR_SIZE;
     const size_t size = type_size(type);
@@ -394,7 +398,7 @@ int ef_norm_backward(ef_workspace *workspace, int64_t rows, int64_t width, int t
 int ef_weight_grad(ef_workspace *workspace, int64_t rows, int64_t out_width, int64_t width, int type, const void *dz,
                    int64_t dz_stride, const void *act, const float *column_scale, float *dw, int accumulate, void *stream)
 {
-    if (!workspace || !dz || !act || !dw) return EF_ERR_NULL;
+    if (!workspace || !dw || missing(rows, dz, act)) return EF_ERR_NULL;
     if (rows < 0 || rows > ROWS_MAX || width < 1 || out_width < 1 || !good_type(type)) return EF_ERR_ARG;
     if (width > WIDTH_MAX || out_width > WIDTH_MAX || rows > workspace->max_rows) return EF_ERR_SIZE;
     const size_t size = type_size(type);
@@ -438,7 +442,7 @@ int ef_weight_grad(ef_workspace *workspace, int64_t rows, int64_t out_width, int
 int ef_token_logp(int64_t rows, int64_t vocab, int type, const void *logits, int64_t stride, const int64_t *tokens, float *logp,
                   void *stream)
 {
-    if (!logp) return EF_ERR_NULL;
+    if (missing(rows, logp)) return EF_ERR_NULL;
     const int rc = policy_args(rows, vocab, type, logits, stride, tokens);
     if (rc) return rc;
     if (!aligned(logp, 4)) return EF_ERR_ALIGN;
@@ -464,7 +468,7 @@ int ef_policy_loss(ef_workspace *workspace, int64_t rows, int64_t vocab, int typ
                    const float *token_weight, float clip_low, float clip_high, float kl, float *logp, float *losses, float *loss,
                    void *dlogits, int64_t dlogits_stride, void *stream)
 {
-    if (!workspace || !advantage || (!logp && !losses && !loss && !dlogits)) return EF_ERR_NULL;
+    if (!workspace || missing(rows, advantage) || (rows && !logp && !losses && !loss && !dlogits)) return EF_ERR_NULL;
     int rc = policy_args(rows, vocab, type, logits, stride, tokens);
     if (rc) return rc;
     if (!(clip_low >= 0.0f && clip_low <= 1.0f) || !(std::isfinite(clip_high) && clip_high >= 0.0f) || !(std::isfinite(kl) && kl >= 0.0f))

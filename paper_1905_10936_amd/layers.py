@@ -11,7 +11,7 @@ import sys
 
 import torch
 
-from . import _check, _f32, _ptr, _stream_ptr, _u8, lib
+from . import EF_ERR_NULL, _check, _f32, _ptr, _stream_ptr, _u8, lib
 
 EF_TYPE_FP32, EF_TYPE_BF16 = 0, 1
 EF_NORM_MAX_WIDTH = 16384
@@ -65,6 +65,16 @@ def _type(t, name):
     return _TYPES[t.dtype]
 
 
+def _required(rows, *given):
+    """Without rows the library takes null for an empty tensor, so what was not given at all is refused here, as it is with rows."""
+    if rows == 0 and any(t is None for t in given):
+        _check(EF_ERR_NULL)
+
+
+def _one_of(*outputs):
+    return next((t for t in outputs if t is not None), None)
+
+
 def _vector(t, n, dtype, name):
     if t is None:
         return None
@@ -95,6 +105,7 @@ def ef_act_encode(x, act, stream=None):
     if rc is not None:
         return _check(rc)
     rows, width = _rows(x, "x")
+    _required(rows, act)
     xp, xs = _matrix(x, (rows, width), x.dtype, "x")
     _check(lib().ef_act_encode(rows, width, _type(x, "x"), xp, xs, _act(act, rows, width), _stream_ptr(stream)))
 
@@ -105,6 +116,7 @@ def ef_act_decode(act, y, stream=None):
     if rc is not None:
         return _check(rc)
     rows, width = _rows(y, "y")
+    _required(rows, act)
     yp, ys = _matrix(y, (rows, width), y.dtype, "y")
     _check(lib().ef_act_decode(rows, width, _act(act, rows, width), _type(y, "y"), yp, ys, _stream_ptr(stream)))
 
@@ -116,6 +128,7 @@ def ef_norm_forward(x, residual, weight, eps, h, y, act, rstd, stream=None):
     if rc is not None:
         return _check(rc)
     shape = _rows(x, "x")
+    _required(shape[0], _one_of(h, y, act, rstd))
     (xp, xs), (rp, rs) = _matrix(x, shape, x.dtype, "x"), _matrix(residual, shape, x.dtype, "residual")
     (hp, hs), (yp, ys) = _matrix(h, shape, x.dtype, "h"), _matrix(y, shape, x.dtype, "y")
     _check(lib().ef_norm_forward(shape[0], shape[1], _type(x, "x"), xp, xs, rp, rs, _vector(weight, shape[1], _f32, "weight"), float(eps),
@@ -170,6 +183,7 @@ def ef_norm_backward(workspace, dy, act, rstd, weight, dh, dx, dweight, accumula
     if rc is not None:
         return _check(rc)
     shape = _rows(dy, "dy")
+    _required(shape[0], act, rstd, dx)
     (gp, gs), (hp, hs) = _matrix(dy, shape, dy.dtype, "dy"), _matrix(dh, shape, dy.dtype, "dh")
     xp, xs = _matrix(dx, shape, dy.dtype, "dx")
     _check(lib().ef_norm_backward(_handle(workspace), shape[0], shape[1], _type(dy, "dy"), gp, gs, _act(act, *shape),
@@ -183,6 +197,7 @@ def ef_weight_grad(workspace, dz, act, column_scale, dw, accumulate=False, strea
     if rc is not None:
         return _check(rc)
     rows, out = _rows(dz, "dz")
+    _required(rows, act)
     if not isinstance(dw, torch.Tensor) or dw.dim() != 2 or dw.shape[0] != out:
         raise TypeError("dw must be 2-D, %d x width" % out)
     width = dw.shape[1]
@@ -198,6 +213,7 @@ def ef_token_logp(logits, tokens, logp, stream=None):
     if rc is not None:
         return _check(rc)
     shape = _rows(logits, "logits")
+    _required(shape[0], tokens, logp)
     lp, ls = _matrix(logits, shape, logits.dtype, "logits")
     _check(lib().ef_token_logp(shape[0], shape[1], _type(logits, "logits"), lp, ls, _vector(tokens, shape[0], torch.int64, "tokens"),
                                _vector(logp, shape[0], _f32, "logp"), _stream_ptr(stream)))
@@ -213,6 +229,7 @@ def ef_policy_loss(workspace, logits, tokens, logp_old, logp_ref, advantage, tok
         return _check(rc)
     shape = _rows(logits, "logits")
     n = shape[0]
+    _required(n, tokens, advantage, _one_of(logp, losses, loss, dlogits))
     (lp, ls), (gp, gs) = _matrix(logits, shape, logits.dtype, "logits"), _matrix(dlogits, shape, logits.dtype, "dlogits")
     _check(lib().ef_policy_loss(_handle(workspace), n, shape[1], _type(logits, "logits"), lp, ls, _vector(tokens, n, torch.int64, "tokens"),
                                 _vector(logp_old, n, _f32, "logp_old"), _vector(logp_ref, n, _f32, "logp_ref"),
