@@ -425,6 +425,8 @@ int ef_act_decode(int64_t rows, int64_t width, const void *act, int type, void *
  *     xhat = v * rstd
  *     h   <- v,  y <- xhat * weight                (each rounded once to `type`)
  *     act <- checkpoint of xhat
+ * Squares are held whatever the size of v: finite rows are normalised from fp32's least
+ * numbers to its largest (rstd itself is infinite where it is beyond fp32).
  * The checkpoint is of the normalised row before the weight: one buffer then
  * serves the norm's backward pass and, with the weight as the columns' factor, the weight
  * gradient of the linear layer that reads y (ef_weight_grad), and neither h nor

@@ -24,13 +24,15 @@ struct NormForward {
     int64_t first;              // the launch's first row
 };
 
+constexpr float NORM_SMALL = 0x1p-80f;      // a sum of squares below has lost some of them to underflow
+
 constexpr int norm_threads(int lanes) { return lanes < 256 ? 256 : lanes; }
 
 template <class T, int LANES, int CHUNKS>
 __global__ __launch_bounds__(norm_threads(LANES)) void k_norm_forward(NormForward a)
 {
     constexpr int TEAMS = norm_threads(LANES) / LANES;
-    __shared__ float sums[LANES > 64 ? LANES / 64 : 1];
+    __shared__ float sums[2][LANES > 64 ? LANES / 64 : 1];
     const int lane = threadIdx.x % LANES;
     const int64_t row = a.first + (int64_t)blockIdx.x * TEAMS + threadIdx.x / LANES;
     if (row >= a.rows) return;          // whole teams; LANES > 64: never
@@ -65,9 +67,27 @@ __global__ __launch_bounds__(norm_threads(LANES)) void k_norm_forward(NormForwar
     for (int c = 0; c < CHUNKS; ++c)
 #pragma unroll
         for (int k = 0; k < 8; ++k) s = __builtin_fmaf(v[c][k], v[c][k], s);
-    s = over_row<Add, LANES>(s, sums);
-    const float rstd = 1.0f / sqrtf(s / (float)a.n + a.eps);
-    if (a.rstd && lane == 0) a.rstd[row] = rstd;
+    s = over_row<Add, LANES>(s, sums[0]);
+    const float mean = s / (float)a.n + a.eps;
+    // xhat = v * before * rstd; `before` is 1 but for a row whose squares fp32 does not hold (from about 10^19 on, or below 10^-12 where eps does not
+    // cover it): they are then taken of v times a power of two, and rstd, which may be out of fp32's range, is kept as two factors that are not.
+    float rstd = 1.0f / sqrtf(mean), before = 1.0f;
+    if (!(mean < INFINITY) || (s < NORM_SMALL && a.eps < NORM_SMALL)) {
+        const bool small = s < NORM_SMALL;
+        const float by = small ? 0x1p100f : 0x1p-72f;
+        s = 0.0f;
+#pragma unroll
+        for (int c = 0; c < CHUNKS; ++c)
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const float t = v[c][k] * by;
+                s = __builtin_fmaf(t, t, s);
+            }
+        s = over_row<Add, LANES>(s, sums[1]);
+        before = small ? 0x1p24f : 0x1p-24f;
+        rstd = 1.0f / sqrtf(s / (float)a.n + a.eps * by * by) * (small ? 0x1p76f : 0x1p-48f);
+    }
+    if (a.rstd && lane == 0) a.rstd[row] = before * rstd;
     if (a.h) {
         T *h = static_cast<T *>(a.h) + row * a.h_stride;
         times<CHUNKS>([&](auto c) {
@@ -76,6 +96,12 @@ __global__ __launch_bounds__(norm_threads(LANES)) void k_norm_forward(NormForwar
             e.round(v[c.value]);
             store_piece<c.value == CHUNKS - 1>(e, h + i, a.n - i);
         });
+    }
+    if (before != 1.0f) {
+#pragma unroll
+        for (int c = 0; c < CHUNKS; ++c)
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[c][k] *= before;
     }
 #pragma unroll
     for (int c = 0; c < CHUNKS; ++c)
