@@ -381,8 +381,8 @@ int ef_compressor_quality_static(const ef_plan *plan, int n_vectors, const float
  * them: fp32, anywhere in the flat d-vector (`weight`, `dweight`, `dw` and the
  * other fp32 vectors of these calls need 4-byte alignment only).
  *
- * Matrices are row-major, one row to a token, `rows` >= 0 of them, of `type`
- * EF_TYPE_FP32 or EF_TYPE_BF16, aligned to their element, rows `*_stride` elements
+ * Matrices are row-major, one row to a token, `rows` of them (0 .. 2^31 - 1, EF_ERR_ARG
+ * otherwise), of `type` EF_TYPE_FP32 or EF_TYPE_BF16, aligned to their element, rows `*_stride` elements
  * apart (>= the row's length; not used and not checked with fewer than two
  * rows).  All calls enqueue on `stream`, allocate nothing, record no memset and
  * may be captured into a HIP graph.  Outputs may share memory neither with each
@@ -409,7 +409,8 @@ int ef_compressor_quality_static(const ef_plan *plan, int n_vectors, const float
  * codes are rounded to nearest even (and held to 448 in size if e ended at 119).  What a
  * checkpoint stands for is therefore a bf16 number exactly.  A group that holds
  * an infinity or NaN gets scale byte 255 and codes that read as NaN.
- * Both functions return 0 for rows < 0, width < 1, or sizes beyond 2^62 bytes.
+ * Both functions return 0 for rows < 0, width < 1, or sizes beyond 2^62 bytes; the calls
+ * take widths up to 2^24 (EF_ERR_SIZE beyond).
  */
 size_t ef_act_bytes(int64_t rows, int64_t width);
 size_t ef_act_scales_offset(int64_t rows, int64_t width);
@@ -489,7 +490,7 @@ int ef_norm_backward(ef_workspace *workspace, int64_t rows, int64_t width, int t
  *   act           in   checkpoint of [rows][width]
  *   column_scale  in   float[width] (the norm's weight where act is ef_norm_forward's), or NULL for ones
  *   dw            out  float[out_width][width], contiguous; accumulate != 0: added to what it holds
- * out_width and width from 1 to 2^24.
+ * out_width and width from 1 to 2^24 (EF_ERR_SIZE beyond).
  */
 int ef_weight_grad(ef_workspace *workspace, int64_t rows, int64_t out_width, int64_t width, int type, const void *dz,
                    int64_t dz_stride, const void *act, const float *column_scale, float *dw, int accumulate, void *stream);

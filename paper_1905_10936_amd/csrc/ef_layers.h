@@ -86,7 +86,8 @@ int on_workspace_device(const ef_workspace *w)
 int act_args(int64_t rows, int64_t width, int type, const void *m, int64_t stride, const void *act)
 {
     if (missing(rows, m, act)) return EF_ERR_NULL;
-    if (rows < 0 || rows > ROWS_MAX || width < 1 || width > WIDTH_MAX || !good_type(type)) return EF_ERR_ARG;
+    if (rows < 0 || rows > ROWS_MAX || width < 1 || !good_type(type)) return EF_ERR_ARG;
+    if (width > WIDTH_MAX) return EF_ERR_SIZE;
     const Matrix a{m, stride, rows, width, type_size(type)};
     if (!a.good_stride()) return EF_ERR_ARG;
     if (!aligned(m, type_size(type)) || !aligned(act, 16)) return EF_ERR_ALIGN;
