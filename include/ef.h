@@ -451,10 +451,11 @@ int ef_norm_forward(int64_t rows, int64_t width, int type, const void *x, int64_
  * Workspace of the calls below: row sums and partial results, no state between
  * calls.  Calls that share one must be ordered on the device and run on the
  * device it was created on (EF_ERR_ARG otherwise).  Takes 64 MiB and
- * 4 bytes a row.  Creation allocates (hipMalloc) and synchronises;
- * ef_workspace_destroy synchronises the device.
+ * 4 bytes a row.  Creation allocates (hipMalloc) on the current device and enqueues
+ * nothing; ef_workspace_destroy waits for the workspace's device, whichever is current.
  *
  *   max_rows  most rows of a later call (EF_ERR_SIZE for more), 0 .. 2^31 - 1
+ *   stream    not used
  */
 typedef struct ef_workspace ef_workspace; /* opaque */
 int ef_workspace_create(ef_workspace **out, int64_t max_rows, void *stream);

@@ -353,8 +353,13 @@ int ef_workspace_create(ef_workspace **out, int64_t max_rows, void *stream)
 int ef_workspace_destroy(ef_workspace *workspace)
 {
     if (!workspace) return EF_ERR_NULL;
+    // on its own device, which need not be the current one
+    int current = workspace->device;
+    (void)hipGetDevice(&current);
+    if (current != workspace->device) (void)hipSetDevice(workspace->device);
     (void)hipDeviceSynchronize();
     (void)hipFree(workspace->base);
+    if (current != workspace->device) (void)hipSetDevice(current);
     delete workspace;
     return EF_OK;
 }

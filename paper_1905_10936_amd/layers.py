@@ -137,7 +137,7 @@ def ef_norm_forward(x, residual, weight, eps, h, y, act, rstd, stream=None):
 
 class Workspace:
     """ef_workspace: room for partial results, for calls of up to max_rows rows on the device that was current at
-    creation.  Calls that share one must be ordered on the device."""
+    creation.  Calls that share one must be ordered on the device.  `stream` is not used."""
 
     def __init__(self, max_rows, stream=None):
         self._h = ctypes.c_void_p()
