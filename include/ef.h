@@ -485,7 +485,7 @@ int ef_norm_backward(ef_workspace *workspace, int64_t rows, int64_t width, int t
  *     dw[o][i] <- [dw[o][i] +] column_scale[i] * sum over rows t of dz[t][o] * act[t][i]
  * on matrix instructions, accumulated in fp32.  What a checkpoint stands for and
  * bf16 gradients enter exactly; fp32 gradients enter as the sum of three bf16 numbers,
- * which holds all their 24 bits (parts below bf16's least normal number, 2^-126, are lost).
+ * which holds all their 24 bits (those below bf16's least number, 2^-133, are cut off).
  *
  *   dz            in   type[rows][dz_stride], rows of out_width
  *   act           in   checkpoint of [rows][width]
