@@ -168,7 +168,9 @@ bool policy_teams(const ef::PolicyArgs &a, hipStream_t s)
 // A row's own arithmetic, a hundred instructions, is a wavefront's whatever the row's length, so short rows are four to a wavefront (32768 rows of 259 in bf16
 // 22 us, 32 with a wavefront to a row; of 600 20 and 31); it costs a workgroup three barriers besides, so a wavefront has rows of up to 4096 or 5120 (16384
 // of 2500 in bf16 41 us, 66 with 256 threads) and a thread of a workgroup many eights where its type lets it (bf16, in us: 8192 x 9000 65 with
-// 256 threads, 99 with 1024; 4096 x 18000 63 and 73; 2048 x 65000 115 with 512, 120 with 1024).  fp32 gains nothing there.
+// 256 threads, 99 with 1024; 4096 x 18000 63 and 73; 2048 x 65000 115 with 512, 120 with 1024).  Between, rows of 24577 to 40960 have 1024 threads: 4 or 5 eights
+// and 64 registers a thread put two workgroups on a CU (8192 x 32768 204, with 512 threads 213, with 256 222; 1024 x 32000 30, 34 and 31; the
+// shortest of them lose, 8192 x 25000 173 and 168; the longest are alike, 4096 x 40000 133 and 134).  fp32 gains nothing from many eights.
 template <class T>
 void policy_rows(const ef::PolicyArgs &a, hipStream_t s)
 {
