@@ -34,7 +34,6 @@ def test_large_and_small_rows(n, dtype):
 
     def make(seed):
         v = rows_of(rows, n, torch.float32, seed).cpu().double() * scale
-        # fp32 input without numbers below the type's normal ones but in the first row, so that a row is what it was
         return v.to(TYPES[dtype]).cuda()
 
     x, r, w = make(n), make(n + 1), 1 + 0.2 * torch.rand(n, device="cuda")
