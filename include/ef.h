@@ -536,6 +536,89 @@ int ef_policy_loss(ef_workspace *workspace, int64_t rows, int64_t vocab, int typ
                    const float *token_weight, float clip_low, float clip_high, float kl, float *logp, float *losses,
                    float *loss, void *dlogits, int64_t dlogits_stride, void *stream);
 
+/*
+ * Gated feed-forward block. w holds both projections, the gate's rows first, then the other's:
+ *     a   = x * w[0 .. inner)^T,   u = x * w[inner .. 2 inner)^T            (accumulated in fp32)
+ *     z  <- act(a) * u,            act(a) = a * sigmoid(F(a))
+ *     pre <- a and u side by side,   act <- checkpoint of z
+ * F(a) = a with EF_GATE_SILU, 2 sqrt(2 / pi) (a + 0.044715 a^3) with EF_GATE_GELU (the tanh form of GELU). z is made from a and u
+ * before they are rounded; z and pre are rounded once to `type`, the checkpoint is of z before that.  The weights are of the activations'
+ * type: a caller that keeps fp32 parameters casts them once a step.  Products of bf16 and of fp32 numbers enter exactly as the
+ * type has them, and are summed in fp32.
+ *
+ *   x    in   type[rows][x_stride], rows of width
+ *   w    in   type[2 * inner][w_stride], rows of width
+ *   pre  out  type[rows][pre_stride], rows of 2 * inner: what ef_gated_backward needs, or NULL
+ *   z    out  type[rows][z_stride], rows of inner, or NULL
+ *   act  out  ef_act_bytes(rows, inner) bytes: for the weight gradient (ef_weight_grad) of the layer that reads z, or NULL
+ * width and inner from 1 to 2^24 (EF_ERR_SIZE beyond); one output at least (EF_ERR_NULL).
+ */
+#define EF_GATE_SILU 0
+#define EF_GATE_GELU 1
+int ef_gated_forward(int64_t rows, int64_t width, int64_t inner, int type, const void *x, int64_t x_stride, const void *w,
+                     int64_t w_stride, int gate, void *pre, int64_t pre_stride, void *z, int64_t z_stride, void *act, void *stream);
+
+/*
+ * Its backward pass. a and u are what pre holds, dz the gradient of z:
+ *     dpre <- dz * u * act'(a) and dz * act(a) side by side   (each rounded once to `type`)
+ *     dx   <- dpre * w                                        (of dpre as it is stored; accumulated in fp32, rounded once)
+ * The weights' gradient, [2 * inner][width] as w, is ef_weight_grad of dpre and the checkpoint of x.
+ *
+ *   dz    in   type[rows][dz_stride], rows of inner
+ *   pre   in   type[rows][pre_stride], rows of 2 * inner, as ef_gated_forward leaves it
+ *   w     in   as there; may be NULL without dx
+ *   dpre  out  type[rows][dpre_stride], rows of 2 * inner; in place over pre
+ *   dx    out  type[rows][dx_stride], rows of width, or NULL
+ */
+int ef_gated_backward(ef_workspace *workspace, int64_t rows, int64_t width, int64_t inner, int type, const void *dz, int64_t dz_stride,
+                      const void *pre, int64_t pre_stride, const void *w, int64_t w_stride, int gate, void *dpre, int64_t dpre_stride,
+                      void *dx, int64_t dx_stride, void *stream);
+
+/*
+ * Draws a token from every row of logits.  A row's entries are ordered by value, downwards, and among equal ones by place, upwards.  With
+ * p_v proportional to exp(logits[t][v] / temperature):
+ *     top_k   keeps the order's first top_k entries                                    (0 or less: all)
+ *     top_p   of those, each whose predecessors have less than top_p of those entries' probability   (1 or more: all; the first always stays)
+ *     min_p   of those, each that has at least min_p times the first one's             (0 or less: all; more than 1 is 1)
+ *     tokens[t] <- the least place at which the probability of what is kept, added up by place, passes uniform[t] of its sum
+ *     logp[t]   <- logits[t][token] - log(sum_v exp(logits[t][v])): the log-probability under the policy itself, without temperature and filters, as
+ *                  ef_token_logp gives it and ef_policy_loss takes it for logp_old
+ * temperature 0, or top_p of 0 or less, takes the order's first entry.  Probabilities are in 64 bits and their sums do not depend on an order:
+ * equal calls draw equal tokens.  -inf rules an entry out.  A row without a distribution gets token -1 and logp NaN: one that holds
+ * a NaN or +inf or nothing but -inf, or whose uniform is not in [0, 1), temperature not finite or below 0, top_p or min_p NaN.  (A token of -1
+ * masks its row in ef_token_logp and ef_policy_loss.)
+ *
+ *   logits       in   as for ef_token_logp
+ *   uniform      in   float[rows], in [0, 1)
+ *   temperature  in   float[rows], or NULL for ones;   top_k  in  int32_t[rows], or NULL;   top_p, min_p  in  float[rows], or NULL
+ *   tokens       out  int64[rows], 8-byte aligned
+ *   logp         out  float[rows], or NULL
+ */
+int ef_sample_tokens(ef_workspace *workspace, int64_t rows, int64_t vocab, int type, const void *logits, int64_t stride,
+                     const float *uniform, const float *temperature, const int32_t *top_k, const float *top_p, const float *min_p,
+                     int64_t *tokens, float *logp, void *stream);
+
+/*
+ * Norm of each worker's gradient over all its tensors, and the clipped gradient in the worker's row of flat gradients, as ef_worker_step
+ * reads it: the tensors one after the other, in their order (the blocks of the plan).  For worker i
+ *     norm[i]    <- sqrt(sum over its tensors of the sum of g^2)               (summed in fp64, in a fixed order)
+ *     flat[i][..] <- g * factor,   factor = max_norm / norm if that is below 1, else 1     (in fp64, rounded to fp32; in place: to the tensor's type)
+ * A worker whose norm is infinite or NaN is not clipped (factor 1): norm tells.  (One beyond fp32 is infinite in norm; the factor goes by the norm itself.)  The call's tensors may have either type and any
+ * alignment to their element.  Everything about them is read on the host during the call; a captured call keeps their addresses.
+ *
+ *   grads     HOST  void *[n_workers][n_tensors]: addresses of device memory, contiguous tensors
+ *   sizes     HOST  int64_t[n_tensors]: their elements, alike for every worker; 0 is allowed
+ *   types     HOST  int[n_tensors]: EF_TYPE_FP32 or EF_TYPE_BF16, alike for every worker
+ *   max_norm  >= 0; infinity: the norm alone, or with flat a copy
+ *   flat      out   float[n_workers][flat_stride] (flat_stride >= the sizes' sum; not used with one worker), what lies behind a row's sum
+ *                   is left as it is; or NULL: the tensors are scaled where they are
+ *   norm      out   float[n_workers]
+ * n_workers >= 1, 0 <= n_tensors <= 2^20; sizes up to 2^50 elements in all (EF_ERR_SIZE beyond, as for more workers than the workspace has
+ * room for, which is above 4000).  What is written may share memory with nothing else of the call (EF_ERR_ARG): in place, every tensor is there once.
+ */
+int ef_grad_clip(ef_workspace *workspace, int n_workers, int64_t n_tensors, void *const *grads, const int64_t *sizes, const int *types,
+                 float max_norm, float *flat, int64_t flat_stride, float *norm, void *stream);
+
 /* Static text for an error code; for EF_ERR_HIP the text of the last HIP error
  * seen by this thread is appended.  The returned pointer stays valid until the
  * same thread calls ef_strerror again. */

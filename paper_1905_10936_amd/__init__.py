@@ -37,6 +37,8 @@ ABI_SYMBOLS = (
     # a worker's forward and backward pass (layers.py)
     "ef_act_bytes", "ef_act_scales_offset", "ef_act_encode", "ef_act_decode", "ef_norm_forward", "ef_norm_backward",
     "ef_workspace_create", "ef_workspace_destroy", "ef_weight_grad", "ef_token_logp", "ef_policy_loss",
+    # what else its step is made of (train.py)
+    "ef_gated_forward", "ef_gated_backward", "ef_sample_tokens", "ef_grad_clip",
 )
 # ... and what include/ef_debug.h declares (tuning and diagnostics the tests use)
 DEBUG_SYMBOLS = (
@@ -85,6 +87,7 @@ def _load_native(L):
                                (module.built_for, _build.binding_built_for()))
         module.bind(*(ctypes.cast(getattr(L, name), ctypes.c_void_p).value for name in _NATIVE_CALLS))
         module.bind_layers(*(ctypes.cast(getattr(L, name), ctypes.c_void_p).value for name in layers.NATIVE_CALLS))
+        module.bind_train(*(ctypes.cast(getattr(L, name), ctypes.c_void_p).value for name in train.NATIVE_CALLS))
     except Exception as e:              # no compiler, another torch or Python, an old file: calls take 1 to 3 us longer
         import warnings
         warnings.warn("%s cannot be used, calls go through ctypes: %s" % (os.path.basename(_build.BINDING), e), RuntimeWarning)
@@ -172,6 +175,7 @@ def lib():
         getattr(L, name).restype = c_int
         getattr(L, name).argtypes = [vp, vp, vp, vp, i64, vp, vp]
     layers.declare(L)
+    train.declare(L)
     L.ef_strerror.restype = ctypes.c_char_p
     L.ef_strerror.argtypes = [c_int]
     _load_native(L)
@@ -582,3 +586,5 @@ from . import layers  # noqa: E402  (it uses the helpers above)
 from .layers import (EF_NORM_MAX_WIDTH, EF_TYPE_BF16, EF_TYPE_FP32, Workspace, ef_act_bytes, ef_act_decode, ef_act_encode,  # noqa: E402,F401
                      ef_act_scales_offset, ef_norm_backward, ef_norm_forward, ef_policy_loss, ef_token_logp, ef_weight_grad,
                      ef_workspace_create, ef_workspace_destroy)
+from . import train  # noqa: E402
+from .train import EF_GATE_GELU, EF_GATE_SILU, ef_gated_backward, ef_gated_forward, ef_grad_clip, ef_sample_tokens  # noqa: E402,F401

@@ -17,7 +17,8 @@ TARGETS = {
     LIB: (os.path.join(CSRC, "ef_api.hip"),
           [os.path.join(CSRC, h) for h in ("ef_device.h", "ef_tile.h", "ef_worker.h", "ef_server.h", "ef_finish.h", "ef_end.h",
                                            "ef_quality.h", "ef_small.h", "ef_layout.h", "ef_layers.h", "ef_rows.h", "ef_act.h",
-                                           "ef_norm.h", "ef_grad.h", "ef_policy.h")] +
+                                           "ef_norm.h", "ef_grad.h", "ef_policy.h", "ef_train.h", "ef_product.h", "ef_gated.h",
+                                           "ef_sample.h", "ef_clip.h")] +
           [os.path.join(ROOT, "include", h) for h in ("ef.h", "ef_debug.h")]),
     BENCH_LIB: (os.path.join(CSRC, "ef_bench.hip"),
                 [os.path.join(CSRC, h) for h in ("ef_tile.h", "ef_layout.h", "ef_probe.h")] +

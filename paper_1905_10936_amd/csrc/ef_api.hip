@@ -1661,6 +1661,7 @@ int ef_state_import(const ef_plan *plan, ef_state *state, const float *mom, cons
 }  // extern "C"
 
 #include "ef_layers.h"
+#include "ef_train.h"
 
 extern "C" {
 

@@ -14,6 +14,7 @@
 #include <climits>
 #include <cstdint>
 #include <cstring>
+#include <vector>
 
 #include "ef.h"
 
@@ -44,6 +45,14 @@ struct LayerEntries {
     decltype(&ef_token_logp) token_logp;
     decltype(&ef_policy_loss) policy_loss;
 } G;
+
+// What else a worker's step is made of (bind_train).
+struct TrainEntries {
+    decltype(&ef_gated_forward) gated_forward;
+    decltype(&ef_gated_backward) gated_backward;
+    decltype(&ef_sample_tokens) sample_tokens;
+    decltype(&ef_grad_clip) grad_clip;
+} H;
 
 // What a Plan or a State knows about itself, packed by Python (no bytes: it is closed).
 struct PlanKey {
@@ -88,7 +97,7 @@ public:
         ok = ok && THPVariable_CheckExact(o);
         if (!ok) return nullptr;
         const at::Tensor &t = THPVariable_Unpack(o);
-        ok = t.defined() && t.is_cuda() && t.is_contiguous();
+        ok = t.defined() && t.is_cuda() && t.is_contiguous() && there(t);
         return ok ? &t : nullptr;
     }
     const at::Tensor *tensor(at::ScalarType type)
@@ -107,7 +116,7 @@ public:
         ok = ok && THPVariable_CheckExact(o);
         if (!ok) return m;
         const at::Tensor &t = THPVariable_Unpack(o);
-        ok = t.defined() && t.is_cuda() && (t.dim() == 1 || t.dim() == 2) && (t.scalar_type() == at::kFloat || t.scalar_type() == at::kBFloat16);
+        ok = t.defined() && t.is_cuda() && (t.dim() == 1 || t.dim() == 2) && (t.scalar_type() == at::kFloat || t.scalar_type() == at::kBFloat16) && there(t);
         if (!ok) return m;
         m.type = t.scalar_type();
         m.rows = t.dim() == 1 ? 1 : t.size(0);
@@ -175,8 +184,13 @@ public:
         return ok ? (void *)c10::hip::getCurrentHIPStream().stream() : nullptr;
     }
     void need(bool condition) { ok = ok && condition; }
+    // from here on tensors have to be on the current device
+    void on_current_device() { device_ = c10::hip::getCurrentHIPStream().device_index(); }
+    PyObject *object() { return next(); }
+    bool there(const at::Tensor &t) const { return device_ < 0 || t.get_device() == device_; }
 
 private:
+    int device_ = -1;
     PyObject *next() { return ok ? a_[i_++] : Py_None; }
     PyObject *const *a_;
     Py_ssize_t i_ = 0;
@@ -554,7 +568,131 @@ PyObject *policy_loss(PyObject *, PyObject *const *a, Py_ssize_t n)
     });
 }
 
-// bind(addresses), bind_layers(addresses): the entry points' addresses, in the order of Entries and of LayerEntries.
+PyObject *gated_forward(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return call(a, n, 7, [](Args &x) {
+        x.on_current_device();
+        const Mat m = x.matrix(), w = x.matrix();
+        const int gate = x.count();
+        x.need(w.width == m.width && w.type == m.type && w.rows % 2 == 0);
+        Mat both = m, half = m;
+        both.width = w.rows;
+        half.width = w.rows / 2;
+        const Mat pre = x.matrix_like(both), z = x.matrix_like(half);
+        void *const act = x.act(m.rows, half.width);
+        void *const s = x.stream();
+        if (!x.ok) return 0;
+        return unlocked([&] {
+            return H.gated_forward(m.rows, m.width, half.width, type_of(m), m.p, m.stride, w.p, w.stride, gate, pre.p, pre.stride, z.p, z.stride, act, s);
+        });
+    });
+}
+
+PyObject *gated_backward(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return call(a, n, 8, [](Args &x) {
+        x.on_current_device();
+        const WorkspaceKey k = x.key<WorkspaceKey>();
+        const Mat dz = x.matrix();
+        Mat both = dz, in = dz;
+        both.width = 2 * dz.width;
+        const Mat pre = x.matrix_like(both), w = x.matrix();
+        const int gate = x.count();
+        in.width = w.width;
+        x.need(w.rows == both.width && w.type == dz.type);
+        const Mat dpre = x.matrix_like(both), dx = x.matrix_like(in);
+        void *const s = x.stream();
+        if (!x.ok) return 0;
+        return unlocked([&] {
+            return H.gated_backward(k.workspace, dz.rows, w.width, dz.width, type_of(dz), dz.p, dz.stride, pre.p, pre.stride, w.p, w.stride, gate, dpre.p,
+                                    dpre.stride, dx.p, dx.stride, s);
+        });
+    });
+}
+
+PyObject *sample_tokens(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return call(a, n, 10, [](Args &x) {
+        x.on_current_device();
+        const WorkspaceKey k = x.key<WorkspaceKey>();
+        const Mat m = x.matrix();
+        const float *uniform = x.row_floats(m.rows), *temperature = x.row_floats(m.rows);
+        const int32_t *top_k = static_cast<const int32_t *>(x.vector(at::kInt, m.rows));
+        const float *top_p = x.row_floats(m.rows), *min_p = x.row_floats(m.rows);
+        int64_t *const tokens = static_cast<int64_t *>(x.vector(at::kLong, m.rows));
+        float *const logp = x.row_floats(m.rows);
+        void *const s = x.stream();
+        if (!x.ok) return 0;
+        return unlocked([&] {
+            return H.sample_tokens(k.workspace, m.rows, m.width, type_of(m), m.p, m.stride, uniform, temperature, top_k, top_p, min_p, tokens, logp, s);
+        });
+    });
+}
+
+// The workers' tensors as a list or tuple of them, or as one of such lists (a worker each).
+PyObject *grad_clip(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return call(a, n, 6, [](Args &x) {
+        x.on_current_device();
+        const WorkspaceKey k = x.key<WorkspaceKey>();
+        PyObject *const list = x.object();
+        const float max_norm = x.number();
+        const auto is_list = [](PyObject *o) { return PyList_CheckExact(o) || PyTuple_CheckExact(o); };
+        x.need(is_list(list) && PySequence_Fast_GET_SIZE(list) > 0);
+        if (!x.ok) return 0;
+        const bool lists = is_list(PySequence_Fast_GET_ITEM(list, 0));
+        const Py_ssize_t workers = lists ? PySequence_Fast_GET_SIZE(list) : 1;
+        x.need(workers <= INT_MAX);
+        std::vector<void *> grads;
+        std::vector<int64_t> sizes;
+        std::vector<int> types;
+        int64_t total = 0;
+        for (Py_ssize_t w = 0; w < workers && x.ok; ++w) {
+            PyObject *const of = lists ? PySequence_Fast_GET_ITEM(list, w) : list;
+            x.need(is_list(of) && (w == 0 || PySequence_Fast_GET_SIZE(of) == (Py_ssize_t)sizes.size()));
+            for (Py_ssize_t i = 0; x.ok && i < PySequence_Fast_GET_SIZE(of); ++i) {
+                PyObject *const o = PySequence_Fast_GET_ITEM(of, i);
+                x.need(THPVariable_CheckExact(o) || THPVariable_Check(o));
+                if (!x.ok) break;
+                const at::Tensor &t = THPVariable_Unpack(o);
+                x.need(t.defined() && t.is_cuda() && t.is_contiguous() && x.there(t) && (t.scalar_type() == at::kFloat || t.scalar_type() == at::kBFloat16));
+                if (!x.ok) break;
+                const int type = t.scalar_type() == at::kFloat ? EF_TYPE_FP32 : EF_TYPE_BF16;
+                if (w == 0) {
+                    sizes.push_back(t.numel());
+                    types.push_back(type);
+                    total += t.numel();
+                }
+                x.need(sizes[i] == t.numel() && types[i] == type);
+                grads.push_back(t.data_ptr());
+            }
+        }
+        // rows of flat may be longer than what goes there
+        float *flat = nullptr;
+        int64_t flat_stride = 0;
+        PyObject *const f = x.object();
+        if (x.ok && f != Py_None) {
+            x.need(THPVariable_CheckExact(f));
+            if (!x.ok) return 0;
+            const at::Tensor &t = THPVariable_Unpack(f);
+            x.need(t.defined() && t.is_cuda() && x.there(t) && t.scalar_type() == at::kFloat && (t.dim() == 1 || t.dim() == 2) && rows(t) == workers &&
+                   t.size(-1) >= total && (t.size(-1) < 2 || t.stride(-1) == 1));
+            if (!x.ok) return 0;
+            flat = f32(&t);
+            flat_stride = stride(t);
+            x.need(flat != nullptr);
+        }
+        float *const norm = x.row_floats(workers);
+        void *const s = x.stream();
+        x.need(norm != nullptr);
+        if (!x.ok) return 0;
+        return unlocked([&] {
+            return H.grad_clip(k.workspace, (int)workers, (int64_t)sizes.size(), grads.data(), sizes.data(), types.data(), max_norm, flat, flat_stride, norm, s);
+        });
+    });
+}
+
+// bind(addresses), bind_layers(addresses), bind_train(addresses): the entry points' addresses, in the order of Entries, LayerEntries and TrainEntries.
 template <class Table>
 PyObject *fill(Table &table, PyObject *const *a, Py_ssize_t n)
 {
@@ -576,6 +714,7 @@ PyObject *fill(Table &table, PyObject *const *a, Py_ssize_t n)
 }
 PyObject *bind(PyObject *, PyObject *const *a, Py_ssize_t n) { return fill(F, a, n); }
 PyObject *bind_layers(PyObject *, PyObject *const *a, Py_ssize_t n) { return fill(G, a, n); }
+PyObject *bind_train(PyObject *, PyObject *const *a, Py_ssize_t n) { return fill(H, a, n); }
 
 #define EF_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {EF_METHOD(bind),
@@ -598,6 +737,11 @@ PyMethodDef methods[] = {EF_METHOD(bind),
                          EF_METHOD(weight_grad),
                          EF_METHOD(token_logp),
                          EF_METHOD(policy_loss),
+                         EF_METHOD(bind_train),
+                         EF_METHOD(gated_forward),
+                         EF_METHOD(gated_backward),
+                         EF_METHOD(sample_tokens),
+                         EF_METHOD(grad_clip),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_ef_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -320,6 +320,13 @@ struct ActRef {
     {
         const unsigned byte = group_scale(v);
         if (LAST && i >= groups * GROUP) return;
+        put_codes<LAST>(row, i, n, v, byte);
+        if (i % GROUP == 0) *scale_at(row, i) = (uint8_t)byte;
+    }
+    // The codes alone, of values whose group has this scale byte.
+    template <bool LAST = true>
+    __device__ __forceinline__ void put_codes(int64_t row, int64_t i, int64_t n, const float *v, unsigned byte) const
+    {
         u32x2 c = codes_of(v, byte);
         if (LAST && byte == SCALE_NAN && i + 8 > n) {       // the padding stays 0
             const int left = (int)max((int64_t)0, n - i);
@@ -328,7 +335,6 @@ struct ActRef {
             c.y &= (unsigned)(keep >> 32);
         }
         *reinterpret_cast<u32x2 *>(code_at(row, i)) = c;
-        if (i % GROUP == 0) *scale_at(row, i) = (uint8_t)byte;
     }
     template <bool LAST = true>
     __device__ __forceinline__ void get(int64_t row, int64_t i, float *v) const

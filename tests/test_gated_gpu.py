@@ -1,0 +1,245 @@
+"""The gated feed-forward block, forward and backward, against its definition in 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+import paper_1905_10936_amd as ef
+from tests import train_oracle as oracle
+
+pytestmark = pytest.mark.gpu
+
+TYPES = {"bf16": torch.bfloat16, "fp32": torch.float32}
+GATES = {"silu": ef.EF_GATE_SILU, "gelu": ef.EF_GATE_GELU}
+# one token to many; channels around the tiles' and words' edges; sums of one product to long ones
+SHAPES = [(1, 1, 1), (1, 1024, 96), (2, 7, 5), (31, 33, 17), (33, 64, 32), (64, 515, 40), (65, 40, 300), (130, 129, 127), (200, 100, 64), (257, 63, 129),
+          (300, 1031, 70), (1000, 72, 260)]
+
+
+def exact(t):
+    return t.double().cpu().numpy()
+
+
+def normal(gen, rows, n, dtype, pad=0, sigma=1.0):
+    t = torch.full((rows, n + pad), float("nan"), device="cuda", dtype=dtype)
+    t[:, :n] = (torch.randn(rows, n, device="cuda", generator=gen) * sigma).to(dtype)
+    return t[:, :n]
+
+
+def within(got, want, off):
+    got = exact(got)
+    assert got.shape == want.shape
+    bad = ~(np.abs(got - want) <= off)
+    assert not bad.any(), (np.argwhere(bad)[:4], got[bad][:4], want[bad][:4], off[bad][:4])
+
+
+def blank(rows, n, dtype, pad=0):
+    return torch.full((rows, n + pad), 7.0, device="cuda", dtype=dtype)
+
+
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("rows,n,f", SHAPES)
+@pytest.mark.parametrize("pad", [0, 5])
+def test_forward(kind, rows, n, f, pad):
+    dtype, gate = TYPES[kind], "gelu" if f % 2 else "silu"
+    gen = torch.Generator("cuda").manual_seed(rows * 7 + n + f + pad)
+    x, w = normal(gen, rows, n, dtype, pad), normal(gen, 2 * f, n, dtype, pad, sigma=1.5 * n ** -0.5)
+    pre, z = blank(rows, 2 * f, dtype, pad), blank(rows, f, dtype, 2 * pad)
+    act = torch.full((ef.ef_act_bytes(rows, f),), 9, dtype=torch.uint8, device="cuda")
+    ef.ef_gated_forward(x, w, GATES[gate], pre[:, :2 * f], z[:, :f], act)
+    z64, pre64, z_raw, z_off, pre_off = oracle.gated_forward(exact(x), exact(w), gate, kind)
+    within(pre[:, :2 * f], pre64, pre_off)
+    within(z[:, :f], z64, z_off)
+    # what lies beside the rows is as it was
+    assert bool((pre[:, 2 * f:] == 7.0).all()) and bool((z[:, f:] == 7.0).all())
+    if kind == "fp32":
+        again = torch.zeros_like(act)
+        ef.ef_act_encode(z[:, :f], again)
+        size = rows * ((f + 31) // 32) * 33
+        assert torch.equal(act[:size], again[:size])
+    else:
+        got = blank(rows, f, torch.float32)
+        ef.ef_act_decode(act, got)
+        # E4M3 to nearest: a sixteenth of the value, or half the least code, 2^-10 of a scale that is at most twice top / 448 up to a power of two
+        top = np.pad(np.abs(z64) + z_raw, ((0, 0), (0, -f % 32))).reshape(rows, -1, 32).max(2).repeat(32, 1)[:, :f]
+        within(got, z64, z_raw + (np.abs(z64) + z_raw) * 2.0 ** -4 + 2.0 ** -10 * np.maximum(top / 224.0, 2.0 ** -116))
+    # each output alone gives the same bits
+    alone = blank(rows, f, dtype)
+    ef.ef_gated_forward(x, w, GATES[gate], None, alone, None)
+    assert torch.equal(alone, z[:, :f])
+    alone = blank(rows, 2 * f, dtype)
+    ef.ef_gated_forward(x, w, GATES[gate], alone, None, None)
+    assert torch.equal(alone, pre[:, :2 * f])
+
+
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("rows,n,f", SHAPES)
+@pytest.mark.parametrize("pad", [0, 3])
+def test_backward(kind, rows, n, f, pad):
+    dtype, gate = TYPES[kind], "silu" if f % 2 else "gelu"
+    gen = torch.Generator("cuda").manual_seed(rows + n * 5 + f + pad)
+    dz, pre, w = normal(gen, rows, f, dtype, pad), normal(gen, rows, 2 * f, dtype, pad, sigma=2.0), normal(gen, 2 * f, n, dtype, pad)
+    dz[::3] = 0                                                     # masked tokens
+    ws = ef.ef_workspace_create(rows)
+    dpre, dx = blank(rows, 2 * f, dtype, pad), blank(rows, n, dtype, pad)
+    ef.ef_gated_backward(ws, dz, pre, w, GATES[gate], dpre[:, :2 * f], dx[:, :n])
+    within(dpre[:, :2 * f], *oracle.gated_slopes(exact(dz), exact(pre), gate, kind))
+    within(dx[:, :n], *oracle.input_grad(exact(dpre[:, :2 * f]), exact(w), kind))
+    assert bool((dpre[:, 2 * f:] == 7.0).all()) and bool((dx[:, n:] == 7.0).all())
+    assert not dx[:, :n][::3].any()
+    # without dx; in place over pre
+    alone = blank(rows, 2 * f, dtype)
+    ef.ef_gated_backward(ws, dz, pre, w, GATES[gate], alone, None)
+    assert torch.equal(alone, dpre[:, :2 * f])
+    again = blank(rows, n, dtype)
+    ef.ef_gated_backward(ws, dz, pre, w, GATES[gate], pre, again)
+    assert torch.equal(pre, dpre[:, :2 * f]) and torch.equal(again, dx[:, :n])
+
+
+@pytest.mark.parametrize("gate", GATES)
+def test_gradients_are_those_of_the_forward_pass(gate):
+    """Differences of the forward pass in fp32 along a direction: (L(x + e d) - L(x - e d)) / 2 e, of which e^2 / 6 of the third derivative and the sums'
+    rounding over e are left."""
+    rows, n, f = 40, 48, 70
+    gen = torch.Generator("cuda").manual_seed(5)
+    x, w, dz = normal(gen, rows, n, torch.float32), normal(gen, 2 * f, n, torch.float32, sigma=n ** -0.5), normal(gen, rows, f, torch.float32)
+    ws = ef.ef_workspace_create(rows)
+    pre, z, dx = blank(rows, 2 * f, torch.float32), blank(rows, f, torch.float32), blank(rows, n, torch.float32)
+    act = torch.zeros(ef.ef_act_bytes(rows, n), dtype=torch.uint8, device="cuda")
+    x_codes = blank(rows, n, torch.float32)
+    ef.ef_act_encode(x, act)
+    ef.ef_act_decode(act, x_codes)
+    x = x_codes                     # what the checkpoint stands for, so that the weights' gradient is exact too
+    ef.ef_gated_forward(x, w, GATES[gate], pre, z, None)
+    dpre, dw = blank(rows, 2 * f, torch.float32), blank(2 * f, n, torch.float32)
+    ef.ef_gated_backward(ws, dz, pre, w, GATES[gate], dpre, dx)
+    ef.ef_weight_grad(ws, dpre, act, None, dw)
+
+    def loss(x, w):
+        z, *_ = oracle.gated_forward(x, w, gate, "fp32")
+        return (z * exact(dz)).sum()
+
+    rng = np.random.default_rng(1)
+    for of, grad in (("x", dx), ("w", dw)):
+        d = rng.standard_normal(tuple(grad.shape))
+        e = 1e-5
+        moved = [loss(exact(x) + s * e * d, exact(w)) if of == "x" else loss(exact(x), exact(w) + s * e * d) for s in (1, -1)]
+        want, got = (moved[0] - moved[1]) / (2 * e), float((exact(grad) * d).sum())
+        size = float((np.abs(exact(grad)) * np.abs(d)).sum())
+        assert abs(got - want) <= 1e-5 * size, of
+
+
+def test_values_out_of_the_ordinary():
+    """Activations whose sigmoid has ended, infinities and NaN: where the formulas take them, in their own rows."""
+    a = torch.tensor([0.0, -0.0, 90.0, -90.0, 1e4, -1e4, 1e18, -1e18, 3e38, -3e38, float("inf"), float("nan"), 1e-40, -1e-40], device="cuda")
+    rows = a.numel()
+    for gate in GATES:
+        x, w = a[:, None].clone(), torch.ones(2, 1, device="cuda")
+        z, pre = blank(rows, 1, torch.float32), blank(rows, 2, torch.float32)
+        ef.ef_gated_forward(x, w, GATES[gate], pre, z, None)
+        assert torch.equal(pre[:10], torch.stack([a, a], 1)[:10])
+        z = z[:, 0].cpu()
+        assert z[0] == 0 and z[1] == 0 and z[2] == 8100.0 and z[4] == 1e8 and z[6] == np.float32(1e18) * np.float32(1e18)
+        assert abs(float(z[3])) < 1e-34 and z[5] == 0 and z[7] == 0 and z[9] == 0 and z[10] == float("inf") and torch.isnan(z[11])
+        ws = ef.ef_workspace_create(rows)
+        dz, dpre = torch.ones(rows, 1, device="cuda"), blank(rows, 2, torch.float32)
+        pre = torch.stack([a, torch.ones_like(a)], 1)
+        ef.ef_gated_backward(ws, dz, pre, w, GATES[gate], dpre, None)
+        d = dpre.cpu()
+        for i, (da, du) in {0: (0.5, 0.0), 2: (1.0, 90.0), 4: (1.0, 1e4), 5: (0.0, 0.0), 7: (0.0, 0.0), 8: (1.0, 3e38), 9: (0.0, 0.0)}.items():
+            assert float(d[i, 0]) == pytest.approx(da, abs=1e-30) and float(d[i, 1]) == pytest.approx(du, rel=1e-6), (gate, i)
+        assert torch.isnan(d[11]).all()
+
+
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("rows", [1, 40, 300])
+def test_a_bad_row_harms_no_other(kind, rows):
+    """NaN in a token's input, and in the weights' row of one channel, stay there; what lies behind a row's end is not read as a number."""
+    dtype, n, f = TYPES[kind], 70, 90
+    gen = torch.Generator("cuda").manual_seed(rows)
+    x, w = normal(gen, rows, n, dtype, 3), normal(gen, 2 * f, n, dtype, 3, sigma=0.1)
+    z, good = blank(rows, f, dtype), blank(rows, f, dtype)
+    ef.ef_gated_forward(x, w, GATES["silu"], None, good, None)
+    w[5, 1] = float("nan")
+    if rows > 1:
+        x[rows // 2, 2] = float("inf")
+    ef.ef_gated_forward(x, w, GATES["silu"], None, z, None)
+    same = torch.ones(rows, f, dtype=torch.bool, device="cuda")
+    same[:, 5] = False
+    if rows > 1:
+        same[rows // 2] = False
+        assert not torch.isfinite(z[rows // 2]).any()
+    assert torch.equal(z[same], good[same]) and bool(torch.isnan(z[:, 5]).all())
+
+
+@pytest.mark.parametrize("rows", [3, 200])
+def test_captured_and_replayed(rows):
+    """On a stream of its own, into a graph; replays beside eager calls, with other inputs in the same buffers."""
+    n, f = 130, 200
+    gen = torch.Generator("cuda").manual_seed(8)
+    x, w, dz = normal(gen, rows, n, torch.bfloat16), normal(gen, 2 * f, n, torch.bfloat16, sigma=0.1), normal(gen, rows, f, torch.bfloat16)
+    ws = ef.ef_workspace_create(rows)
+    pre, z, dpre, dx = (blank(rows, k, torch.bfloat16) for k in (2 * f, f, 2 * f, n))
+
+    def step():
+        ef.ef_gated_forward(x, w, GATES["gelu"], pre, z, None)
+        ef.ef_gated_backward(ws, dz, pre, w, GATES["gelu"], dpre, dx)
+
+    stream, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    with torch.cuda.stream(stream):
+        step()
+        torch.cuda.synchronize()
+        with torch.cuda.graph(graph, stream=stream):
+            step()
+    for seed in range(3):
+        x.copy_(normal(gen, rows, n, torch.bfloat16))
+        dz.copy_(normal(gen, rows, f, torch.bfloat16))
+        step()
+        want = [t.clone() for t in (pre, z, dpre, dx)]
+        for t in (pre, z, dpre, dx):
+            t.fill_(3.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        for t, v in zip((pre, z, dpre, dx), want):
+            assert torch.equal(t, v)
+
+
+def test_long_sums_and_many_parts():
+    """Few tokens, many channels summed over: the backward product is cut along them."""
+    rows, n, f = 96, 200, 5000
+    for kind, dtype in TYPES.items():
+        gen = torch.Generator("cuda").manual_seed(3)
+        dz, pre, w = normal(gen, rows, f, dtype), normal(gen, rows, 2 * f, dtype), normal(gen, 2 * f, n, dtype, sigma=0.01)
+        ws = ef.ef_workspace_create(rows)
+        dpre, dx, again = blank(rows, 2 * f, dtype), blank(rows, n, dtype), blank(rows, n, dtype)
+        ef.ef_gated_backward(ws, dz, pre, w, GATES["silu"], dpre, dx)
+        within(dx, *oracle.input_grad(exact(dpre), exact(w), kind))
+        ws.close()
+        ws = ef.ef_workspace_create(rows)
+        ef.ef_gated_backward(ws, dz, pre, w, GATES["silu"], dpre, again)
+        assert torch.equal(dx, again)
+
+
+@pytest.mark.parametrize("kind", TYPES)
+def test_large_tiles(kind):
+    """Enough rows and channels for the largest tiles; a sample of the results in 64 bits."""
+    rows, n, f = (3001, 328, 2100) if kind == "bf16" else (3001, 200, 2100)
+    dtype = TYPES[kind]
+    gen = torch.Generator("cuda").manual_seed(12)
+    x, w = normal(gen, rows, n, dtype), normal(gen, 2 * f, n, dtype, sigma=n ** -0.5)
+    pre, z = blank(rows, 2 * f, dtype), blank(rows, f, dtype)
+    ef.ef_gated_forward(x, w, GATES["silu"], pre, z, None)
+    some = np.r_[0:5, 250:260, 2990:3001]
+    z64, pre64, _, z_off, pre_off = oracle.gated_forward(exact(x)[some], exact(w), "silu", kind)
+    within(z[some], z64, z_off)
+    within(pre[some], pre64, pre_off)
+    few = [blank(5, k, dtype) for k in (2 * f, f)]
+    ef.ef_gated_forward(x[:5], w, GATES["silu"], few[0], few[1], None)
+    within(few[1], z64[:5], z_off[:5])
+    ws = ef.ef_workspace_create(20000)
+    rows, n, f = 20000, 700, 130
+    dz, pre, w = normal(gen, rows, f, dtype), normal(gen, rows, 2 * f, dtype), normal(gen, 2 * f, n, dtype)
+    dpre, dx = blank(rows, 2 * f, dtype), blank(rows, n, dtype)
+    ef.ef_gated_backward(ws, dz, pre, w, GATES["gelu"], dpre, dx)
+    some = np.r_[0:5, 250:260, 19990:20000]
+    within(dx[some], *oracle.input_grad(exact(dpre[some]), exact(w), kind))
+    within(dpre[some], *oracle.gated_slopes(exact(dz[some]), exact(pre[some]), "gelu", kind))
