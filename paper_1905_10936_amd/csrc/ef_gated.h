@@ -29,14 +29,22 @@ struct GatedArgs {
 
 constexpr float GELU_SLOPE = 1.5957691216057308f, GELU_CUBIC = 0.044715f;      // 2 sqrt(2 / pi)
 
-// sigmoid(F(a)) and 1 - sigmoid(F(a)), from exp(-|F(a)|) so that neither loses what the other one rounds away.  The bf16 block takes the instruction's exponential:
-// its exponent's rounding, |F| 2^-24, is far below half a step of what is stored wherever the sigmoid is not.
+// sigmoid(F(a)) and 1 - sigmoid(F(a)), from exp(-|F(a)|) so that neither loses what the other one rounds away.  The bf16 block takes the instructions'
+// exponential and reciprocal: their errors and the exponent's rounding, |F| 2^-24, are far below half a step of what is stored wherever the sigmoid is
+// not.  (With a division and expf a tile of 256 tokens by 128 channels spends 13 us behind its products, 4 this way.)
 template <class T>
 __device__ __forceinline__ float2 sigmoid(float a, int gate)
 {
-    const float s = gate == GATE_GELU ? GELU_SLOPE * (a + GELU_CUBIC * a * a * a) : a;
-    const float e = sizeof(T) == 2 ? __builtin_amdgcn_exp2f(-fabsf(s) * 1.44269504f) : expf(-fabsf(s));
-    const float big = 1.0f / (1.0f + e), small = e * big;
+    const float s = gate == GATE_GELU ? GELU_SLOPE * __builtin_fmaf(GELU_CUBIC * a * a, a, a) : a;
+    float e, big;
+    if constexpr (sizeof(T) == 2) {
+        e = __builtin_amdgcn_exp2f(-1.44269504f * fabsf(s));
+        big = __builtin_amdgcn_rcpf(1.0f + e);
+    } else {
+        e = expf(-fabsf(s));
+        big = 1.0f / (1.0f + e);
+    }
+    const float small = e * big;
     return s < 0.0f ? make_float2(small, big) : make_float2(big, small);        // a NaN goes on: both are NaN
 }
 template <class T>
@@ -48,18 +56,6 @@ __device__ __forceinline__ int2 tile_place(int id, int all, int tiles_t, int til
     id = id % 8 * (all / 8) + min(id % 8, all % 8) + id / 8;
     const int group = id / (8 * tiles_c), in = id % (8 * tiles_c), high = min(8, tiles_t - group * 8);
     return make_int2(group * 8 + in % high, in / high);
-}
-
-// Eight consecutive channels of a token in each lane: lanes l < 32 get those from 16 p + 0 on, lanes l + 32 those from 16 p + 8 on, from runs 2 p and 2 p + 1 of
-// four of an accumulator's lane.
-__device__ __forceinline__ void runs_together(const float *run0, const float *run1, float *v)
-{
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        const u32x2 t = __builtin_amdgcn_permlane32_swap(__float_as_uint(run0[k]), __float_as_uint(run1[k]), false, false);
-        v[k] = __uint_as_float(t.x);
-        v[4 + k] = __uint_as_float(t.y);
-    }
 }
 
 template <class T, int WC, int WT>
@@ -95,62 +91,67 @@ __global__ __launch_bounds__(PRODUCT_THREADS, WC * WT > 4 ? 1 : 2) void k_gated(
             b.load_guarded(g.x, g.x_stride, step * STEP<T>, g.n, x_row);
         });
 
+    using Rows = StagedRows<T, 32 * PAIRS>;
+    static_assert(3 * 4 * Rows::BYTES <= (int)sizeof lds, "three results of four wavefronts");
+    char *const mine = lds + wave * 3 * Rows::BYTES;
+    const auto ending = [&](auto inside) {
+        constexpr bool INSIDE = decltype(inside)::value;
+        const int64_t c1 = c0 + wave_c * PAIRS * 32, left = g.f - c1;
+        if (!INSIDE && left <= 0) return;
 #pragma unroll
-    for (int j = 0; j < WT; ++j) {
-        const int64_t t = t0 + (wave_t * WT + j) * 32 + lane % 32;
-        const bool there = t < g.rows;
+        for (int j = 0; j < WT; ++j) {
+            const int64_t t1 = t0 + (wave_t * WT + j) * 32, rows = g.rows - t1;
+            if (!INSIDE && rows <= 0) return;
+            const bool there = INSIDE || lane % 32 < rows;
 #pragma unroll
-        for (int i = 0; i < PAIRS; ++i) {
-            const int64_t block = c0 + (wave_c * PAIRS + i) * 32;
-            if (block >= g.f) continue;         // the same for the wavefront
-            float z[2][8];
+            for (int i = 0; i < PAIRS; ++i) {
+                float z[2][8];
 #pragma unroll
-            for (int p = 0; p < 2; ++p) {
-                float va[8], vu[8], first[4], second[4];
-                const int64_t c = block + 16 * p + lane / 32 * 8;
-                const auto both = [&](const f32x16 &m, float *v) {
+                for (int p = 0; p < 2; ++p) {
+                    float va[8], vu[8];
+                    const int c = 32 * i + 16 * p + lane / 32 * 8;
+                    eight_channels(acc[i][j], p, va);
+                    eight_channels(acc[i + PAIRS][j], p, vu);
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        first[k] = m[8 * p + k];
-                        second[k] = m[8 * p + 4 + k];
+                    for (int k = 0; k < 8; ++k) z[p][k] = gated<T>(va[k], vu[k], g.gate);
+                    if (g.z) Rows::put(mine, lane, c, z[p]);
+                    if (g.pre) {
+                        Rows::put(mine + Rows::BYTES, lane, c, va);
+                        Rows::put(mine + 2 * Rows::BYTES, lane, c, vu);
                     }
-                    runs_together(first, second, v);
-                };
-                both(acc[i][j], va);
-                both(acc[i + PAIRS][j], vu);
-                Eight<T> e;
-                if (g.pre && there) {
-                    T *const row = static_cast<T *>(g.pre) + t * g.pre_stride + c;
-                    e.round(va);
-                    store_some(e, row, g.f - c);
-                    e.round(vu);
-                    store_some(e, row + g.f, g.f - c);
                 }
+                if (g.act.codes && (INSIDE || 32 * i < left)) {
+                    // a group of 32 channels: lanes l and l + 32, sixteen values each
+                    unsigned top = 0;
 #pragma unroll
-                for (int k = 0; k < 8; ++k) z[p][k] = c + k < g.f ? gated<T>(va[k], vu[k], g.gate) : 0.0f;
-                if (g.z && there) {
-                    e.round(z[p]);
-                    store_some(e, static_cast<T *>(g.z) + t * g.z_stride + c, g.f - c);
+                    for (int p = 0; p < 2; ++p)
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) {
+                            if (!INSIDE && 32 * i + 16 * p + lane / 32 * 8 + k >= left) z[p][k] = 0.0f;
+                            top = larger(top, __float_as_uint(z[p][k]) & 0x7fffffffu);
+                        }
+                    const u32x2 s = __builtin_amdgcn_permlane32_swap(top, top, false, false);
+                    const unsigned byte = scale_byte(__uint_as_float(larger(s.x, s.y)));
+                    if (there) {
+                        const int64_t t = t1 + lane % 32;
+#pragma unroll
+                        for (int p = 0; p < 2; ++p) g.act.template put_codes<!INSIDE>(t, c1 + 32 * i + 16 * p + lane / 32 * 8, g.f, z[p], byte);
+                        if (lane < 32) *g.act.scale_at(t, c1 + 32 * i) = (uint8_t)byte;
+                    }
                 }
             }
-            if (g.act.codes) {
-                // a group of 32 channels: lanes l and l + 32, sixteen values each
-                unsigned top = 0;
-#pragma unroll
-                for (int k = 0; k < 8; ++k) top = larger(top, larger(__float_as_uint(z[0][k]) & 0x7fffffffu, __float_as_uint(z[1][k]) & 0x7fffffffu));
-                const u32x2 s = __builtin_amdgcn_permlane32_swap(top, top, false, false);
-                const unsigned byte = scale_byte(__uint_as_float(larger(s.x, s.y)));
-                if (there) {
-#pragma unroll
-                    for (int p = 0; p < 2; ++p) {
-                        const int64_t c = block + 16 * p + lane / 32 * 8;
-                        g.act.put_codes(t, c, g.f, z[p], byte);
-                    }
-                    if (lane < 32) *g.act.scale_at(t, block) = (uint8_t)byte;
-                }
+            if (g.z) Rows::template flush<INSIDE>(mine, lane, static_cast<T *>(g.z) + t1 * g.z_stride + c1, g.z_stride, rows, left);
+            if (g.pre) {
+                T *const to = static_cast<T *>(g.pre) + t1 * g.pre_stride + c1;
+                Rows::template flush<INSIDE>(mine + Rows::BYTES, lane, to, g.pre_stride, rows, left);
+                Rows::template flush<INSIDE>(mine + 2 * Rows::BYTES, lane, to + g.f, g.pre_stride, rows, left);
             }
         }
-    }
+    };
+    if (t0 + TILE_T <= g.rows && c0 + TILE_C <= g.f)
+        ending(std::true_type());
+    else
+        ending(std::false_type());
 }
 
 // Few tokens: bound by the weights' bytes.  A workgroup takes CHANNELS = 16 or 32 channels of the product (both projections) and up to 32 tokens, its wavefronts the steps in turn;
@@ -321,33 +322,41 @@ __global__ __launch_bounds__(PRODUCT_THREADS, WC * WT > 4 ? 1 : 2) void k_input_
             a.load_guarded(g.w, g.w_stride, step * STEP<T>, g.k, c0, g.n);
             b.load_guarded(g.dpre, g.dpre_stride, step * STEP<T>, g.k, row);
         });
+    const auto ending = [&](auto inside, auto of, auto *to, int64_t stride) {
+        constexpr bool INSIDE = decltype(inside)::value;
+        using Rows = StagedRows<decltype(of), 32 * WC>;
+        static_assert(4 * Rows::BYTES <= (int)sizeof lds, "of four wavefronts");
+        char *const mine = lds + wave * Rows::BYTES;
+        const int64_t c1 = c0 + wave_c * WC * 32, left = g.n - c1;
+        if (!INSIDE && left <= 0) return;
 #pragma unroll
-    for (int j = 0; j < WT; ++j) {
-        const int64_t t = t0 + (wave_t * WT + j) * 32 + lane % 32;
+        for (int j = 0; j < WT; ++j) {
+            const int64_t t1 = t0 + (wave_t * WT + j) * 32, rows = g.rows - t1;
+            if (!INSIDE && rows <= 0) return;
 #pragma unroll
-        for (int i = 0; i < WC; ++i) {
+            for (int i = 0; i < WC; ++i)
 #pragma unroll
-            for (int p = 0; p < 2; ++p) {
-                float v[8], one[4], two[4];
-                const int64_t c = c0 + (wave_c * WC + i) * 32 + 16 * p + lane / 32 * 8;
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    one[k] = acc[i][j][8 * p + k];
-                    two[k] = acc[i][j][8 * p + 4 + k];
+                for (int p = 0; p < 2; ++p) {
+                    float v[8];
+                    eight_channels(acc[i][j], p, v);
+                    Rows::put(mine, lane, 32 * i + 16 * p + lane / 32 * 8, v);
                 }
-                runs_together(one, two, v);
-                if (t >= g.rows) continue;
-                if (g.splits > 1) {
-                    Eight<float> e;
-                    e.round(v);
-                    store_some(e, g.parts + ((int64_t)split * g.rows + t) * g.n + c, g.n - c);
-                } else {
-                    Eight<T> e;
-                    e.round(v);
-                    store_some(e, static_cast<T *>(g.dx) + t * g.dx_stride + c, g.n - c);
-                }
-            }
+            Rows::template flush<INSIDE>(mine, lane, to + t1 * stride + c1, stride, rows, left);
         }
+    };
+    const bool inside = t0 + TILE_T <= g.rows && c0 + TILE_C <= g.n;
+    if (g.splits > 1) {
+        float *const to = g.parts + (int64_t)split * g.rows * g.n;
+        if (inside)
+            ending(std::true_type(), float(), to, g.n);
+        else
+            ending(std::false_type(), float(), to, g.n);
+    } else {
+        T *const to = static_cast<T *>(g.dx);
+        if (inside)
+            ending(std::true_type(), T(), to, g.dx_stride);
+        else
+            ending(std::false_type(), T(), to, g.dx_stride);
     }
 }
 

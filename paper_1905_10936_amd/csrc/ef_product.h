@@ -174,11 +174,14 @@ __device__ __forceinline__ void multiply(const u32x4 &a, const u32x4 &b, f32x16 
 
 // The products of steps first .. last - 1 into acc.  begin(): the operands to step `first`; next(): to the step behind the one that they stand at;
 // guarded(step): that step's words with zeros in the place of what is not there.  Steps from `safe` on are loaded by guarded() alone.
+//
+// As in the weight gradient: fragments are read a region ahead, words of the next step go to LDS one by one behind the products and are asked for again for the step
+// behind that; one barrier a step, before its last region, which reads the next step's first fragments.
 template <class T, int WC, int WT, class A, class B, class Next, class Guarded>
 __device__ __forceinline__ void product_steps(A &a, B &b, char *lds, int64_t first, int64_t last, int64_t safe, int wave_c, int wave_t,
                                               f32x16 (&acc)[WC][WT], Next advance, Guarded guarded)
 {
-    constexpr int BYTES = A::BYTES + B::BYTES;
+    constexpr int BYTES = A::BYTES + B::BYTES, PRODUCTS = WC * WT, READS = WC * A::HALVES + WT * B::HALVES, PIECES = A::N + B::N;
     const int lane = threadIdx.x % 64;
     const int a_at = A::lane_at(lane), b_at = B::lane_at(lane);
 #pragma unroll
@@ -187,52 +190,154 @@ __device__ __forceinline__ void product_steps(A &a, B &b, char *lds, int64_t fir
         for (int j = 0; j < WT; ++j)
 #pragma unroll
             for (int k = 0; k < 16; ++k) acc[i][j][k] = 0.0f;
+    u32x4 fa[2][WC], fb[2][WT];
+    // read q of region r's fragments
+    const auto read = [&](const char *buffer, int r, int q) {
+        if (q < WC * A::HALVES)
+            A::fragment(fa[r & 1][q / A::HALVES], buffer, a_at, wave_c * WC + q / A::HALVES, r, q % A::HALVES);
+        else
+            B::fragment(fb[r & 1][(q - WC * A::HALVES) / B::HALVES], buffer + A::BYTES, b_at, wave_t * WT + (q - WC * A::HALVES) / B::HALVES, r,
+                        (q - WC * A::HALVES) % B::HALVES);
+    };
+    const auto product = [&](int r, int m) { multiply<T>(fa[r & 1][m / WT], fb[r & 1][m % WT], acc[m / WT][m % WT]); };
+    const auto put = [&](char *buffer, int q) {
+        if (q < A::N)
+            a.put(q, buffer);
+        else
+            b.put(q - A::N, buffer + A::BYTES);
+    };
+    const auto load = [&](int q) {
+        if (q < A::N)
+            a.load(q);
+        else
+            b.load(q - A::N);
+    };
     char *now = lds, *next = lds + BYTES;
-    const auto load = [&](int64_t step) {
-        if (step < safe) {
-#pragma unroll
-            for (int i = 0; i < A::N; ++i) a.load(i);
-#pragma unroll
-            for (int i = 0; i < B::N; ++i) b.load(i);
-            advance();
-        } else {
-            guarded(step);
-        }
-    };
-    const auto put = [&](char *buffer) {
-#pragma unroll
-        for (int i = 0; i < A::N; ++i) a.put(i, buffer);
-#pragma unroll
-        for (int i = 0; i < B::N; ++i) b.put(i, buffer + A::BYTES);
-    };
-    if (first < last) {
-        load(first);
-        put(now);
-    }
-    __syncthreads();
-    for (int64_t step = first; step < last; ++step) {
-        if (step + 1 < last) load(step + 1);
-#pragma unroll
-        for (int r = 0; r < REGIONS; ++r) {
-            u32x4 fa[WC], fb[WT];
-#pragma unroll
-            for (int i = 0; i < WC; ++i)
-#pragma unroll
-                for (int h = 0; h < A::HALVES; ++h) A::fragment(fa[i], now, a_at, wave_c * WC + i, r, h);
-#pragma unroll
-            for (int j = 0; j < WT; ++j)
-#pragma unroll
-                for (int h = 0; h < B::HALVES; ++h) B::fragment(fb[j], now + A::BYTES, b_at, wave_t * WT + j, r, h);
-#pragma unroll
-            for (int i = 0; i < WC; ++i)
-#pragma unroll
-                for (int j = 0; j < WT; ++j) multiply<T>(fa[i], fb[j], acc[i][j]);
-        }
-        if (step + 1 < last) put(next);
-        __syncthreads();
+    const auto turn = [&] {
         char *t = now;
         now = next;
         next = t;
+    };
+    int64_t step = first;
+    if (first < last) {
+        if (first < safe) {
+#pragma unroll
+            for (int q = 0; q < PIECES; ++q) load(q);
+            advance();
+        } else {
+            guarded(first);
+        }
+#pragma unroll
+        for (int q = 0; q < PIECES; ++q) put(now, q);
+        if (first + 1 < safe) {
+#pragma unroll
+            for (int q = 0; q < PIECES; ++q) load(q);
+            if (first + 2 < safe) advance();
+        }
+    }
+    __syncthreads();
+    if (step + 1 < safe) {
+#pragma unroll
+        for (int q = 0; q < READS; ++q) read(now, 0, q);
+        for (; step + 1 < safe; ++step) {
+            times<REGIONS * PRODUCTS>([&](auto slot) {
+                constexpr int r = slot.value / PRODUCTS, m = slot.value % PRODUCTS;
+                constexpr GradSchedule<REGIONS, PRODUCTS, READS, PIECES> PLAN;
+                if constexpr (slot.value == (REGIONS - 1) * PRODUCTS) __syncthreads();
+                product(r, m);
+                times<PLAN.reads[m + 1] - PLAN.reads[m]>([&](auto q) { read(r < REGIONS - 1 ? now : next, (r + 1) % REGIONS, PLAN.reads[m] + q.value); });
+                times<PLAN.piece[slot.value + 1] - PLAN.piece[slot.value]>([&](auto q) {
+                    put(next, PLAN.piece[slot.value] + q.value);
+                    load(PLAN.piece[slot.value] + q.value);
+                });
+                __builtin_amdgcn_sched_barrier(0);
+            });
+            // the words then hold the step behind the next, the same words again where there is no such step
+            if (step + 3 < safe) advance();
+            turn();
+        }
+    }
+    // what is left: the step in LDS, and those that load() may not take
+    for (; step < last; ++step) {
+        if (step + 1 < last) guarded(step + 1);
+#pragma unroll
+        for (int r = 0; r < REGIONS; ++r) {
+#pragma unroll
+            for (int q = 0; q < READS; ++q) read(now, r, q);
+#pragma unroll
+            for (int m = 0; m < PRODUCTS; ++m) product(r, m);
+        }
+        if (step + 1 < last) {
+#pragma unroll
+            for (int q = 0; q < PIECES; ++q) put(next, q);
+        }
+        __syncthreads();
+        turn();
+    }
+}
+
+// Results of a wavefront on their way to memory by LDS, 32 tokens of CHANNELS channels: a store then takes whole rows, not 32 bytes of each of 32 rows
+// (8192 tokens, 1024 -> 4096 channels in bf16 with both projections kept: 242 us with stores from the accumulators, 162 this way and with the
+// cheaper sigmoid).
+template <class T, int CHANNELS>
+struct StagedRows {
+    static constexpr int PITCH = CHANNELS * (int)sizeof(T) + 16, BYTES = 32 * PITCH, CHUNKS = CHANNELS / WORD<T>, EACH = 64 / CHUNKS;
+    // eight channels from c on of the lane's token
+    static __device__ __forceinline__ void put(char *at, int lane, int c, const float *v)
+    {
+        Eight<T> e;
+        e.round(v);
+        char *const p = at + lane % 32 * PITCH + c * (int)sizeof(T);
+        if constexpr (sizeof(T) == 2) {
+            *reinterpret_cast<u32x4 *>(p) = e.w;
+        } else {
+            *reinterpret_cast<u32x4 *>(p) = e.lo;
+            *reinterpret_cast<u32x4 *>(p + 16) = e.hi;
+        }
+    }
+    // rows of `stride` from `to` on; with INSIDE all of them are there, else `rows` of them and `left` channels of a row
+    template <bool INSIDE>
+    static __device__ __forceinline__ void flush(const char *at, int lane, T *to, int64_t stride, int64_t rows, int64_t left)
+    {
+        const int chunk = lane % CHUNKS, row = lane / CHUNKS;
+        to += row * stride + chunk * WORD<T>;
+        at += row * PITCH + chunk * 16;
+        if constexpr (INSIDE) {
+            u32x4 w[32 / EACH];
+#pragma unroll
+            for (int i = 0; i < 32 / EACH; ++i) w[i] = *reinterpret_cast<const u32x4 *>(at + i * EACH * PITCH);
+#pragma unroll
+            for (int i = 0; i < 32 / EACH; ++i) {
+                if constexpr (sizeof(T) == 2)
+                    *(EF_GLOBAL u32x4_any *)(EF_GLOBAL T *)(to + i * EACH * stride) = w[i];
+                else
+                    *(EF_GLOBAL u32x4_word *)(EF_GLOBAL T *)(to + i * EACH * stride) = w[i];
+            }
+        } else {
+            const int n = (int)min((int64_t)WORD<T>, left - chunk * WORD<T>);
+            for (int i = 0; i < 32 / EACH && i * EACH + row < rows; ++i, to += EACH * stride, at += EACH * PITCH) {
+                if (n == WORD<T>) {
+                    if constexpr (sizeof(T) == 2)
+                        *(EF_GLOBAL u32x4_any *)(EF_GLOBAL T *)to = *reinterpret_cast<const u32x4 *>(at);
+                    else
+                        *(EF_GLOBAL u32x4_word *)(EF_GLOBAL T *)to = *reinterpret_cast<const u32x4 *>(at);
+                } else {
+                    for (int k = 0; k < n; ++k) to[k] = reinterpret_cast<const T *>(at)[k];
+                }
+            }
+        }
+    }
+};
+
+// Eight consecutive channels of a token in each lane: lanes l < 32 get those from 16 p on, lanes l + 32 those from 16 p + 8 on, from runs 2 p and 2 p + 1 of four of
+// an accumulator's lane.
+__device__ __forceinline__ void eight_channels(const f32x16 &acc, int p, float *v)
+{
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const u32x2 t = __builtin_amdgcn_permlane32_swap(__float_as_uint(acc[8 * p + k]), __float_as_uint(acc[8 * p + 4 + k]), false, false);
+        v[k] = __uint_as_float(t.x);
+        v[4 + k] = __uint_as_float(t.y);
     }
 }
 
