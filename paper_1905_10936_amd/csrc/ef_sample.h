@@ -1,18 +1,20 @@
 // Drawing tokens from rows of logits: temperature, top-k, top-p, min-p, and a given random number a row.
 //
-// The order of a row's entries is by value, downwards, then by place.  Every filter keeps a beginning of that order, so what is kept is told by a
-// key (the value as an ordered whole number) and how many of the entries at that key stay, the first ones by place.  Both are found a byte of the
-// key at a time from a histogram: of numbers of entries for top-k, of probability for top-p.
+// The order of a row's entries is by value, downwards, then by place.  Every filter keeps a beginning of that order, so what is kept is told by its last
+// entry, a value and a place.  Top-k's is found from a histogram of the values, linear in the value and not in its bits (logits are spread over few powers of two: bins of
+// bits would have a wavefront's atomics meet in one), and the order within the one bin where the count runs out; top-p's the same way by probability.  A bin with
+// too many entries is binned again between its least and largest value; one of a single value is settled by counting places.
 //
 // Probabilities are 2^((v - top) log2(e) / T) in 64 bits, rounded to multiples of a power of two so large that sums of a whole row are exact (SampleRow::grid): they
-// come out the same in whatever order they are added, and by LDS atomics too.  In fp32 a draw next to a border would go by the order of the sums.
+// come out the same in whatever order they are added, by LDS atomics too.  In fp32 one draw in 300 over 50000 entries would go by the order of the sums.
+// Sums and draws look only at what is kept; a team reads its row once and keeps it in LDS.
 #pragma once
 #include "ef_rows.h"
 
 namespace ef {
 
 struct SampleArgs {
-    int64_t rows, vocab;
+    int64_t first, rows, vocab;         // of this launch: rows from `first` on
     const void *logits;
     int64_t stride;
     const float *uniform, *temperature;
@@ -21,8 +23,6 @@ struct SampleArgs {
     int64_t *tokens;
     float *logp;
 };
-
-constexpr int SAMPLE_THREADS = 1024, SAMPLE_WAVES = SAMPLE_THREADS / 64;
 
 // 2^x for x <= 0 in 64 bits, to 1e-11 of it; 0 below 2^-60.
 __device__ __forceinline__ double power_of_two(double x)
@@ -42,7 +42,7 @@ __device__ __forceinline__ double power_of_two(double x)
     return x >= -60.0 ? __builtin_amdgcn_ldexp(p, (int)r) : 0.0;
 }
 
-// A value as a whole number of the same order; -0 is 0.
+// A value as a whole number of the same order; 0 and -0 are one.
 __device__ __forceinline__ unsigned key_of(float v)
 {
     const unsigned b = __float_as_uint(v + 0.0f);
@@ -72,288 +72,452 @@ __device__ __forceinline__ V upto_lane(V v, int lane)
     return v;
 }
 
-struct SampleShared {
-    double mass[256], wave_mass[SAMPLE_WAVES];
-    unsigned count[256], wave_count[SAMPLE_WAVES];
-    float wave_top[SAMPLE_WAVES];
-    unsigned key, bad;
-    unsigned rank, ties;        // of what top-k or top-p look for: entries of it to keep, entries there are
-    double above;
-    int64_t place;
-};
-
-// Sums over the workgroup; every thread gets the result.
-__device__ __forceinline__ double over_workgroup(double v, double *at)
-{
-    const int lane = threadIdx.x % 64;
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) v += from_lane(v, lane ^ d);
-    __syncthreads();
-    if (lane == 0) at[threadIdx.x / 64] = v;
-    __syncthreads();
-    double s = 0.0;
-    for (int i = 0; i < SAMPLE_WAVES; ++i) s += at[i];
-    return s;
-}
-
-// One row.  Wavefront w has the elements from w * span on, in eights, 512 at a time, so that places ascend with the wavefront, the round and the lane.
-template <class T>
-struct SampleRow {
-    const T *l;
-    int64_t vocab, span;
-    float top;
-    double factor, grid;        // log2(e) / T; what makes (w + grid) - grid a multiple of a power of two
-
-    __device__ __forceinline__ double weight(float v) const { return power_of_two(((double)v - (double)top) * factor); }
-    __device__ __forceinline__ double mass(float v) const { return (weight(v) + grid) - grid; }
-    // f(values, place of the first, how many there are) for every eight of the calling wavefront
-    template <class F>
-    __device__ __forceinline__ void each(F f) const
+// LANES threads that have a row: a wavefront, or the whole workgroup.
+template <int LANES>
+struct Team {
+    static constexpr int WAVES = LANES / 64, THREADS = LANES < 256 ? 256 : LANES, TEAMS = THREADS / LANES;
+    static constexpr int BINS = LANES == 64 ? 512 : 2048, LISTED = LANES == 64 ? 64 : 512;
+    struct Shared {
+        double bins[BINS], wave_sum[WAVES], sorted_weight[LISTED], above;
+        uint64_t list[LISTED], sorted[LISTED];
+        int64_t place;
+        unsigned wave_count[WAVES], listed, least, most, bin, key, bad;
+        float wave_top[WAVES];
+    };
+    static __device__ __forceinline__ void sync()
     {
-        const int64_t begin = (int64_t)(threadIdx.x / 64) * span, end = min(vocab, begin + span);
-        for (int64_t i = begin; i < end; i += 512) {
-            const int64_t at = i + threadIdx.x % 64 * 8;
-            Eight<T> e;
-            load_some(e, l + at, end - at, sizeof(T) == 2 ? 0xff80ff80u : 0xff800000u);
-            f(e, at, (int)max((int64_t)0, min((int64_t)8, end - at)));
+        if constexpr (LANES == 64) {
+            // a wavefront's LDS operations are carried out in their order
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+        } else {
+            __syncthreads();
         }
+    }
+    // Sum over the team's threads up to this one, and over all of them.
+    static __device__ __forceinline__ double upto(double v, double *at, double &all)
+    {
+        const int lane = threadIdx.x % 64;
+        v = upto_lane(v, lane);
+        if constexpr (LANES == 64) {
+            all = from_lane(v, 63);
+        } else {
+            sync();
+            if (lane == 63) at[threadIdx.x / 64] = v;
+            sync();
+            all = 0.0;
+            double before = 0.0;
+#pragma unroll
+            for (int i = 0; i < WAVES; ++i) {
+                if (i == (int)threadIdx.x / 64) before = all;
+                all += at[i];
+            }
+            v += before;
+        }
+        return v;
     }
 };
 
 template <class T>
-__global__ __launch_bounds__(SAMPLE_THREADS) void k_sample(SampleArgs a)
+__device__ __forceinline__ float largest(const Eight<T> &e)
 {
-    __shared__ SampleShared s;
-    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-    const int64_t row = blockIdx.x;
+    return fmaxf(fmaxf(fmaxf(e[0], e[1]), fmaxf(e[2], e[3])), fmaxf(fmaxf(e[4], e[5]), fmaxf(e[6], e[7])));
+}
+
+// A row that a team looks through again and again: in LDS as it lies in memory where HELD elements hold it, else from the caches.  Wavefront w has the elements from
+// w * span on, 512 to a round: places ascend with the wavefront, the round and the lane.
+template <class T, int LANES, int HELD>
+struct SampleRow {
+    const T *l;
+    T *held;
+    int64_t vocab, begin, end;
+    static constexpr unsigned NONE = sizeof(T) == 2 ? 0xff80ff80u : 0xff800000u;        // -inf
+
+    // f(eight, place of its first element) for every eight of the thread: rounds of 64 of them, what lies behind the row's end is -inf
+    template <class F>
+    __device__ __forceinline__ void each(F f) const
+    {
+        if constexpr (HELD) {
+            for (int i = (int)begin; i < (int)end; i += 512) {
+                const int at = i + threadIdx.x % 64 * 8;
+                Eight<T> e;
+                const u32x4 *p = reinterpret_cast<const u32x4 *>(held + at);
+                if constexpr (sizeof(T) == 2) {
+                    e.w = p[0];
+                } else {
+                    e.lo = p[0];
+                    e.hi = p[1];
+                }
+                f(e, (int64_t)at);
+            }
+        } else {
+            from_memory(f);
+        }
+    }
+    template <class F>
+    __device__ __forceinline__ void from_memory(F f) const
+    {
+        constexpr int AHEAD = 4;
+        for (int64_t i = begin; i < end; i += AHEAD * 512) {
+            Eight<T> e[AHEAD];
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k) {
+                const int64_t at = i + k * 512 + threadIdx.x % 64 * 8;
+                load_some(e[k], l + at, end - at, NONE);
+            }
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k)
+                if (i + k * 512 < end) f(e[k], i + k * 512 + threadIdx.x % 64 * 8);
+        }
+    }
+    __device__ __forceinline__ SampleRow(const T *row, T *buffer, int64_t n)
+    {
+        const int64_t span = ((n + LANES / 64 - 1) / (LANES / 64) + 511) / 512 * 512;
+        l = row;
+        held = buffer;
+        vocab = n;
+        begin = (int64_t)(threadIdx.x % LANES / 64) * span;
+        end = min(n, begin + span);
+    }
+    // The first time through: to LDS besides.
+    template <class F>
+    __device__ __forceinline__ void load(F f)
+    {
+        from_memory([&](const Eight<T> &e, int64_t at) {
+            if constexpr (HELD) {
+                u32x4 *p = reinterpret_cast<u32x4 *>(held + at);
+                if constexpr (sizeof(T) == 2) {
+                    p[0] = e.w;
+                } else {
+                    p[0] = e.lo;
+                    p[1] = e.hi;
+                }
+            }
+            f(e, at);
+        });
+    }
+};
+
+template <class T, int LANES, int HELD>
+struct Sampler {
+    using Of = Team<LANES>;
+    typename Of::Shared &s;
+    SampleRow<T, LANES, HELD> row;
+    float top;
+    double factor, grid;        // log2(e) / T; what makes (w + grid) - grid a multiple of a power of two
+    // kept: larger than `least`, or equal to it and at most at `last`
+    float least;
+    int64_t last;
+
+    __device__ __forceinline__ double weight(float v) const { return power_of_two(((double)v - (double)top) * factor); }
+    __device__ __forceinline__ double mass(float v) const { return (weight(v) + grid) - grid; }
+    // f(value, place) of everything kept
+    template <class F>
+    __device__ __forceinline__ void each_kept(F f) const
+    {
+        row.each([&](const Eight<T> &e, int64_t at) {
+            if (largest(e) >= least) {
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    if (e[k] > least || (e[k] == least && at + k <= last)) f(e[k], at + k);
+            }
+        });
+    }
+    static __device__ __forceinline__ int bin_of(float v, double origin, double scale)
+    {
+        return (int)fmin((origin - (double)v) * scale, (double)(Of::BINS - 1));
+    }
+    __device__ __forceinline__ void clear_bins()
+    {
+        Of::sync();
+#pragma unroll
+        for (int k = 0; k < Of::BINS / LANES; ++k) s.bins[threadIdx.x % LANES + k * LANES] = 0.0;
+        if (threadIdx.x % LANES == 0) {
+            s.listed = s.most = 0;
+            s.least = 0xffffffffu;
+        }
+        Of::sync();
+    }
+    // The bin in which the sums from the first one on reach the target, which `target_of` makes of the sum of all of them: s.bin, and in s.above `above` with
+    // all bins before it.  Returns false where the target is not below that sum, unless it is known to be reached.
+    template <class F>
+    __device__ __forceinline__ bool find_bin(double above, F target_of, double &target, bool reached = false)
+    {
+        constexpr int PER = Of::BINS / LANES;
+        Of::sync();
+        const int first = threadIdx.x % LANES * PER;
+        double own[PER], sum = 0.0, all;
+#pragma unroll
+        for (int k = 0; k < PER; ++k) {
+            own[k] = s.bins[first + k];
+            sum += own[k];
+        }
+        double before = Of::upto(sum, s.wave_sum, all) - sum + above;
+        target = target_of(all);
+        if (!reached && target >= all) return false;
+#pragma unroll
+        for (int k = 0; k < PER; ++k) {
+            if (before < target && before + own[k] >= target) {
+                s.bin = first + k;
+                s.above = before;
+            }
+            before += own[k];
+        }
+        Of::sync();
+        return true;
+    }
+
+    // Keeps, of what is kept, the beginning whose weights reach a target: all entries before which there is less.
+    template <class W, class F>
+    __device__ __forceinline__ void cut(double range, W weight_of, F target_of)
+    {
+        double origin = top, scale = Of::BINS / range, above = 0.0, target = 0.0;
+        float low = least, high = top;
+        for (int level = 0;; ++level) {
+            clear_bins();
+            each_kept([&](float v, int64_t) {
+                if (v >= low && v <= high) unsafeAtomicAdd(&s.bins[bin_of(v, origin, scale)], weight_of(v));
+            });
+            // from the second level on it is a bin that reaches the target which is taken apart
+            if (!find_bin(above, [&](double all) { return level == 0 ? target_of(all) : target; }, target, level > 0)) return;
+            above = s.above;
+            const int bin = (int)s.bin;
+            each_kept([&](float v, int64_t at) {
+                if (v >= low && v <= high && bin_of(v, origin, scale) == bin) {
+                    const unsigned key = key_of(v);
+                    const unsigned long long here = __ballot(1);
+                    const int lane = threadIdx.x % 64, leader = __builtin_ctzll(here);
+                    unsigned n = 0;
+                    if (lane == leader) n = atomicAdd(&s.listed, (unsigned)__builtin_popcountll(here));
+                    n = (unsigned)__builtin_amdgcn_readlane((int)n, leader) + (unsigned)__builtin_popcountll(here & ((1ull << lane) - 1));
+                    if (n < Of::LISTED) s.list[n] = (uint64_t)~key << 32 | (uint64_t)(unsigned)at;
+                    atomicMin(&s.least, key);
+                    atomicMax(&s.most, key);
+                }
+            });
+            Of::sync();
+            const unsigned listed = s.listed, lo = s.least, hi = s.most;
+            if (listed <= Of::LISTED) {
+                in_list((int)listed, above, target, weight_of);
+                return;
+            }
+            low = value_of(lo);
+            high = value_of(hi);
+            if (lo == hi) {
+                in_places(low, listed, above, target, weight_of(low));
+                return;
+            }
+            origin = high;
+            scale = Of::BINS / ((double)high - (double)low);
+        }
+    }
+
+    // The cut within the listed entries: each finds its rank among them, and the sum of weights up to it.
+    template <class W>
+    __device__ __forceinline__ void in_list(int n, double above, double target, W weight_of)
+    {
+        const int i = threadIdx.x % LANES;
+        if (i < n) {
+            const uint64_t mine = s.list[i];
+            int rank = 0;
+            for (int j = 0; j < n; ++j) rank += s.list[j] < mine;
+            s.sorted[rank] = mine;
+            s.sorted_weight[rank] = weight_of(value_of(~(unsigned)(mine >> 32)));
+        }
+        Of::sync();
+        const double w = i < n ? s.sorted_weight[i] : 0.0;
+        double all;
+        const double sum = above + Of::upto(w, s.wave_sum, all), before = sum - w;
+        // the last one before which there is less than the target; the first of the bin is one
+        if (i < n && before < target && (i == n - 1 || sum >= target)) {
+            s.key = ~(unsigned)(s.sorted[i] >> 32);
+            s.place = (int64_t)(unsigned)s.sorted[i];
+        }
+        Of::sync();
+        least = value_of(s.key);
+        last = s.place;
+    }
+
+    // The cut among `n` entries of one value, each of weight w.
+    __device__ __forceinline__ void in_places(float value, unsigned n, double above, double target, double w)
+    {
+        double j = __builtin_floor((target - above) / w);
+        j = fmin(fmax(j, 0.0), (double)n);
+        while (j < (double)n && above + j * w < target) j += 1.0;
+        while (j > 1.0 && above + (j - 1.0) * w >= target) j -= 1.0;
+        const unsigned rank = (unsigned)fmax(j, 1.0);
+        const int lane = threadIdx.x % 64, wave = threadIdx.x % LANES / 64;
+        const float was_least = least;
+        const int64_t was_last = last;
+        // those already cut off stand behind all that are kept
+        const auto there = [&](const Eight<T> &e, int64_t at, int k) { return e[k] == value && (value > was_least || at + k <= was_last); };
+        unsigned mine = 0;
+        row.each([&](const Eight<T> &e, int64_t at) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) mine += there(e, at, k);
+        });
+        const unsigned sum = upto_lane(mine, lane);
+        Of::sync();
+        if (lane == 63) s.wave_count[wave] = sum;
+        Of::sync();
+        unsigned before = 0;
+        int in = 0;
+        while (in < Of::WAVES - 1 && before + s.wave_count[in] < rank) before += s.wave_count[in++];
+        if (wave == in) {
+            row.each([&](const Eight<T> &e, int64_t at) {
+                unsigned here = 0;
+#pragma unroll
+                for (int k = 0; k < 8; ++k) here += there(e, at, k);
+                const unsigned upto = upto_lane(here, lane);
+                unsigned c = before + upto - here;
+                if (c < rank && before + upto >= rank) {
+#pragma unroll
+                    for (int k = 0; k < 8; ++k)
+                        if (there(e, at, k) && ++c == rank) s.place = at + k;
+                }
+                before += from_lane(upto, 63);
+            });
+        }
+        Of::sync();
+        least = value;
+        last = s.place;
+    }
+
+    // Of few entries all but about those are left out at once: k threads' largest values are k entries, so that what is below the least of them cannot be among
+    // the first k.
+    __device__ __forceinline__ void leave_out(int64_t k, float mine)
+    {
+        if (k > LANES / 2) return;
+        const double origin = top, scale = Of::BINS / 24.0;
+        clear_bins();
+        const bool some = mine >= least;
+        const int bin = some ? bin_of(mine, origin, scale) : Of::BINS;
+        if (some) unsafeAtomicAdd(&s.bins[bin], 1.0);
+        double target;
+        if (!find_bin(0.0, [&](double) { return (double)k; }, target)) return;
+        if (bin <= (int)s.bin) atomicMin(&s.least, key_of(mine));
+        Of::sync();
+        least = value_of(s.least);
+    }
+};
+
+template <class T, int LANES, int HELD>
+__global__ __launch_bounds__(Team<LANES>::THREADS) void k_sample(SampleArgs a)
+{
+    using Of = Team<LANES>;
+    __shared__ typename Of::Shared shared[Of::TEAMS];
+    const int lane = threadIdx.x % 64, wave = threadIdx.x % LANES / 64;
+    const int64_t row = a.first + (int64_t)blockIdx.x * Of::TEAMS + (Of::TEAMS > 1 ? threadIdx.x / LANES : 0);
+    if (row >= a.rows) return;          // whole wavefronts, which meet no other
+    typename Of::Shared &s = shared[Of::TEAMS > 1 ? threadIdx.x / LANES : 0];
+    __shared__ __align__(16) T held[Of::TEAMS][HELD ? HELD : 8];
+    Sampler<T, LANES, HELD> r{s, {static_cast<const T *>(a.logits) + row * a.stride, held[Of::TEAMS > 1 ? threadIdx.x / LANES : 0], a.vocab}};
     const float u = a.uniform[row], heat = a.temperature ? a.temperature[row] : 1.0f;
     const float top_p = a.top_p ? a.top_p[row] : 1.0f, min_p = a.min_p ? a.min_p[row] : 0.0f;
     const int64_t top_k = a.top_k ? a.top_k[row] : 0;
-    SampleRow<T> r;
-    r.l = static_cast<const T *>(a.logits) + row * a.stride;
-    r.vocab = a.vocab;
-    r.span = ((a.vocab + SAMPLE_WAVES - 1) / SAMPLE_WAVES + 511) / 512 * 512;
 
     // ---- the largest value; what is no distribution
-    if (threadIdx.x == 0) s.bad = 0;
-    float top = -INFINITY;
+    float mine = -INFINITY;
     bool bad = false;
-    r.each([&](const Eight<T> &e, int64_t, int n) {
+    r.row.load([&](const Eight<T> &e, int64_t) {
+        mine = fmaxf(mine, largest(e));
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            top = fmaxf(top, e[k]);
-            bad = bad || e[k] != e[k];
-        }
+        for (int k = 0; k < 8; ++k) bad = bad || e[k] != e[k];
     });
-    top = over_lanes<Max, 64>(top);
-    __syncthreads();
-    if (lane == 0) s.wave_top[wave] = top;
-    if (bad) s.bad = 1;
-    __syncthreads();
-    for (int i = 0; i < SAMPLE_WAVES; ++i) top = fmaxf(top, s.wave_top[i]);
+    float top = over_lanes<Max, 64>(mine);
+    bad = __any(bad);
+    if constexpr (LANES > 64) {
+        if (lane == 0) s.wave_top[wave] = bad ? NAN : top;
+        Of::sync();
+#pragma unroll
+        for (int i = 0; i < Of::WAVES; ++i) {
+            const float t = s.wave_top[i];
+            bad = bad || t != t;
+            top = fmaxf(top, t);
+        }
+    }
     // one comparison to each, false for a NaN
-    const bool good = !s.bad && top > -INFINITY && top < INFINITY && u >= 0.0f && u < 1.0f && heat >= 0.0f && heat < INFINITY && top_p == top_p &&
-                      min_p == min_p;
+    const bool good = !bad && top > -INFINITY && top < INFINITY && u >= 0.0f && u < 1.0f && heat >= 0.0f && heat < INFINITY && top_p == top_p && min_p == min_p;
     if (!good) {
-        if (threadIdx.x == 0) {
+        if (threadIdx.x % LANES == 0) {
             a.tokens[row] = -1;
             if (a.logp) a.logp[row] = NAN;
         }
         return;
     }
     r.top = top;
-    const unsigned top_key = key_of(top);
+    r.least = -3.402823466e38f;
+    r.last = INT64_MAX;
     // The sum of the row's masses stays below 2^52 times their grid.
     r.grid = __builtin_amdgcn_ldexp(1.5, 64 - __builtin_clzll((unsigned long long)a.vocab));
-    const bool greedy = heat == 0.0f || top_p <= 0.0f;
-    r.factor = 1.4426950408889634074;
-    double whole = 0.0;         // at temperature 1
+    // The policy's own sum, in fp32's exponentials: a term's error is its own, and the sums are in 64 bits.
+    double whole = 0.0;
     if (a.logp) {
-        r.each([&](const Eight<T> &e, int64_t, int) {
+        r.row.each([&](const Eight<T> &e, int64_t) {
+            float v[8];
 #pragma unroll
-            for (int k = 0; k < 8; ++k) whole += r.weight(e[k]);
+            for (int k = 0; k < 8; ++k) v[k] = __builtin_amdgcn_exp2f((e[k] - top) * 1.44269504f);
+            whole += (double)(((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7])));
         });
-        whole = over_workgroup(whole, s.wave_mass);
+        double all;
+        Of::upto(whole, s.wave_sum, all);
+        whole = all;
     }
+
+    // ---- what is kept
+    const bool greedy = heat == 0.0f || top_p <= 0.0f;
+    const int64_t k = greedy ? 1 : top_k;
     r.factor = greedy ? 0.0 : 1.4426950408889634074 / (double)heat;
-
-    // ---- what is kept: keys above `key`, and the first `rank` entries at it
-    unsigned key = 0, rank = 0xffffffffu, ties = 0xffffffffu;
-    constexpr int BYTES = sizeof(T);        // a bf16 value's key ends in two bytes that its first two tell
-    if (greedy) {
-        key = top_key;
-        rank = 1;
-    } else if (top_k > 0 && top_k < a.vocab) {
-        unsigned left = (unsigned)top_k, prefix = 0;
-        for (int b = 3; b >= 4 - BYTES; --b) {
-            const unsigned mask = b == 3 ? 0u : 0xffffffffu << 8 * (b + 1);
-            __syncthreads();
-            if (threadIdx.x < 256) s.count[threadIdx.x] = 0;
-            __syncthreads();
-            r.each([&](const Eight<T> &e, int64_t, int n) {
-#pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    const unsigned q = key_of(e[k]);
-                    if (k < n && (q & mask) == prefix) atomicAdd(&s.count[q >> 8 * b & 255], 1u);
-                }
-            });
-            __syncthreads();
-            if (threadIdx.x == 0) {
-                int i = 255;
-                unsigned more = left;
-                for (; s.count[i] < more; --i) more -= s.count[i];
-                s.key = prefix | (unsigned)i << 8 * b;
-                s.rank = more;
-                s.ties = s.count[i];
-            }
-            __syncthreads();
-            prefix = s.key;
-            left = s.rank;
-        }
-        key = sizeof(T) == 2 && !(prefix & 0x80000000u) ? prefix | 0xffffu : prefix;
-        rank = left;
-        ties = s.ties;
+    if (k > 0 && k < a.vocab) {
+        r.leave_out(k, mine);
+        r.cut(24.0, [](float) { return 1.0; }, [&](double) { return (double)k; });
     }
-    if (!greedy && top_p < 1.0f) {
-        double total = 0.0;
-        r.each([&](const Eight<T> &e, int64_t, int) {
-#pragma unroll
-            for (int k = 0; k < 8; ++k)
-                if (key_of(e[k]) > key) total += r.mass(e[k]);
-        });
-        total = over_workgroup(total, s.wave_mass);
-        if (rank != 0xffffffffu) total += r.mass(value_of(key)) * (double)rank;
-        const double target = (double)top_p * total;
-        double above = 0.0;
-        unsigned prefix = 0;
-        for (int b = 3; b >= 4 - BYTES; --b) {
-            const unsigned mask = b == 3 ? 0u : 0xffffffffu << 8 * (b + 1);
-            __syncthreads();
-            if (threadIdx.x < 256) {
-                s.mass[threadIdx.x] = 0.0;
-                s.count[threadIdx.x] = 0;
-            }
-            __syncthreads();
-            r.each([&](const Eight<T> &e, int64_t, int n) {
-#pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    const unsigned q = key_of(e[k]);
-                    if (k < n && q >= key && (q & mask) == prefix) {
-                        unsafeAtomicAdd(&s.mass[q >> 8 * b & 255], r.mass(e[k]));
-                        atomicAdd(&s.count[q >> 8 * b & 255], 1u);
-                    }
-                }
-            });
-            __syncthreads();
-            if (threadIdx.x == 0) {
-                // the first group that brings the mass to the target; it has mass of its own
-                int i = 255, found = -1;
-                double sum = above;
-                for (; i >= 0; --i) {
-                    if (s.mass[i] > 0.0) {
-                        found = i;
-                        s.above = sum;
-                        if (sum + s.mass[i] >= target) break;
-                        sum += s.mass[i];
-                    }
-                }
-                s.key = prefix | (unsigned)found << 8 * b;
-                s.ties = s.count[found];
-            }
-            __syncthreads();
-            prefix = s.key;
-            above = s.above;
-        }
-        const unsigned found = sizeof(T) == 2 && !(prefix & 0x80000000u) ? prefix | 0xffffu : prefix;
-        const unsigned most = found == key && rank != 0xffffffffu ? rank : s.ties;
-        // entries at the key while the mass before them is below the target
-        const double w = r.mass(value_of(found));
-        double j = __builtin_floor((target - above) / w);
-        j = fmin(fmax(j, 0.0), (double)most);
-        while (j < (double)most && above + j * w < target) j += 1.0;
-        while (j > 1.0 && above + (j - 1.0) * w >= target) j -= 1.0;
-        key = found;
-        rank = (unsigned)fmax(j, 1.0);
-        ties = s.ties;
-    }
-
-    // ---- where the last of the entries at the key stands
-    int64_t last = a.vocab;
-    if (rank < ties) {
-        unsigned mine = 0;
-        r.each([&](const Eight<T> &e, int64_t, int n) {
-#pragma unroll
-            for (int k = 0; k < 8; ++k) mine += k < n && key_of(e[k]) == key;
-        });
-        const unsigned sum = upto_lane(mine, lane);
-        __syncthreads();
-        if (lane == 63) s.wave_count[wave] = sum;
-        __syncthreads();
-        unsigned before = 0;
-        int in = 0;
-        while (in < SAMPLE_WAVES - 1 && before + s.wave_count[in] < rank) before += s.wave_count[in++];
-        if (wave == in) {
-            r.each([&](const Eight<T> &e, int64_t at, int n) {
-                unsigned here = 0;
-#pragma unroll
-                for (int k = 0; k < 8; ++k) here += k < n && key_of(e[k]) == key;
-                const unsigned upto = upto_lane(here, lane);
-                unsigned c = before + upto - here;
-                if (c < rank && before + upto >= rank) {
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) {
-                        if (k < n && key_of(e[k]) == key && ++c == rank) s.place = at + k;
-                    }
-                }
-                before += from_lane(upto, 63);
-            });
-        }
-        __syncthreads();
-        last = s.place;
-    }
+    if (!greedy && top_p < 1.0f)
+        r.cut(fmin(24.0 * (double)heat, 1e30), [&](float v) { return r.mass(v); }, [&](double all) { return (double)top_p * all; });
+    const double floor_p = fmin((double)min_p, 1.0);
+    const auto kept_mass = [&](float v) {
+        const double w = r.weight(v);
+        return w >= floor_p ? (w + r.grid) - r.grid : 0.0;
+    };
 
     // ---- the draw: the first entry with more than u of the kept mass up to it
-    const double least = fmin((double)min_p, 1.0);
-    const auto kept = [&](float v, int64_t at) {
-        const unsigned q = key_of(v);
-        if (q < key || (q == key && at > last)) return 0.0;
-        const double w = r.weight(v);
-        return w >= least ? (w + r.grid) - r.grid : 0.0;
-    };
-    double mine = 0.0;
-    r.each([&](const Eight<T> &e, int64_t at, int n) {
+    double own = 0.0;
+    r.each_kept([&](float v, int64_t) { own += kept_mass(v); });
+    const double upto = upto_lane(own, lane);
+    double total = 0.0, before = 0.0;
+    if constexpr (LANES > 64) {
+        Of::sync();
+        if (lane == 63) s.wave_sum[wave] = upto;
+        Of::sync();
 #pragma unroll
-        for (int k = 0; k < 8; ++k)
-            if (k < n) mine += kept(e[k], at + k);
-    });
-    const double upto = upto_lane(mine, lane);
-    __syncthreads();
-    if (lane == 63) s.wave_mass[wave] = upto;
-    __syncthreads();
-    double total = 0.0;
-    for (int i = 0; i < SAMPLE_WAVES; ++i) total += s.wave_mass[i];
+        for (int i = 0; i < Of::WAVES; ++i) total += s.wave_sum[i];
+    } else {
+        total = from_lane(upto, 63);
+    }
     const double target = (double)u * total;
-    double before = 0.0;
-    int in = 0;
-    while (in < SAMPLE_WAVES - 1 && before + s.wave_mass[in] <= target) before += s.wave_mass[in++];
-    if (wave != in) return;
-    r.each([&](const Eight<T> &e, int64_t at, int n) {
-        double here = 0.0;
+    if constexpr (LANES > 64) {
+        int in = 0;
+        while (in < Of::WAVES - 1 && before + s.wave_sum[in] <= target) before += s.wave_sum[in++];
+        if (wave != in) return;
+    }
+    r.row.each([&](const Eight<T> &e, int64_t at) {
+        if (!__any(largest(e) >= r.least)) return;
+        double m[8], here = 0.0;
 #pragma unroll
-        for (int k = 0; k < 8; ++k)
-            if (k < n) here += kept(e[k], at + k);
+        for (int k = 0; k < 8; ++k) {
+            m[k] = e[k] > r.least || (e[k] == r.least && at + k <= r.last) ? kept_mass(e[k]) : 0.0;
+            here += m[k];
+        }
         const double sum = upto_lane(here, lane);
         double c = before + (sum - here);
         if (c <= target && before + sum > target) {
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
-                if (k >= n) break;
-                const double m = kept(e[k], at + k);
-                if (c <= target && c + m > target) {
+                if (c <= target && c + m[k] > target) {
                     a.tokens[row] = at + k;
                     if (a.logp) a.logp[row] = (float)(((double)e[k] - (double)top) - log(whole));
                 }
-                c += m;
+                c += m[k];
             }
         }
         before += from_lane(sum, 63);

@@ -69,6 +69,32 @@ void launch_input_grad(const ef::InputGradArgs &a, hipStream_t s)
         launch_input_grad<T, 2, 2>(a, s);
 }
 
+template <class T, int LANES, int HELD>
+void launch_sample(ef::SampleArgs a, hipStream_t s)
+{
+    using Of = ef::Team<LANES>;
+    in_launches(ceil_div(a.rows, Of::TEAMS), [&](dim3 grid, int64_t first) {
+        a.first = first * Of::TEAMS;
+        hipLaunchKernelGGL((ef::k_sample<T, LANES, HELD>), grid, dim3(Of::THREADS), 0, s, a);
+    });
+}
+// A wavefront takes rows of up to 2048, a workgroup longer ones: in 48 KB of LDS, which leaves room for a second one on the CU, in 128 KB, or from the caches.
+template <class T>
+void launch_sample(const ef::SampleArgs &a, hipStream_t s)
+{
+    constexpr int KB = 1024 / (int)sizeof(T);
+    if (a.vocab <= 512)
+        launch_sample<T, 64, 512>(a, s);
+    else if (a.vocab <= 2048)
+        launch_sample<T, 64, 2048>(a, s);
+    else if (a.vocab <= 48 * KB)
+        launch_sample<T, 1024, 48 * KB>(a, s);
+    else if (a.vocab <= 128 * KB)
+        launch_sample<T, 1024, 128 * KB>(a, s);
+    else
+        launch_sample<T, 1024, 0>(a, s);
+}
+
 int gated_sizes(int64_t rows, int64_t width, int64_t inner, int type, int gate)
 {
     if (rows < 0 || rows > ROWS_MAX || width < 1 || inner < 1 || !good_type(type) || (gate != EF_GATE_SILU && gate != EF_GATE_GELU)) return EF_ERR_ARG;
@@ -158,9 +184,8 @@ int ef_sample_tokens(ef_workspace *workspace, int64_t rows, int64_t vocab, int t
     if (!apart(out, 2, in, 6, in_place)) return EF_ERR_ARG;
     rc = on_workspace_device(workspace);
     if (rc || !rows) return rc;
-    if (rows > GRID_MAX) return EF_ERR_SIZE;
-    const ef::SampleArgs a{rows, vocab, logits, stride, uniform, temperature, top_k, top_p, min_p, tokens, logp};
-    EF_BY_TYPE(type, T, hipLaunchKernelGGL(ef::k_sample<T>, dim3((unsigned)rows), dim3(ef::SAMPLE_THREADS), 0, static_cast<hipStream_t>(stream), a));
+    const ef::SampleArgs a{0, rows, vocab, logits, stride, uniform, temperature, top_k, top_p, min_p, tokens, logp};
+    EF_BY_TYPE(type, T, launch_sample<T>(a, static_cast<hipStream_t>(stream)));
     EF_HIP(hipGetLastError());
     return EF_OK;
 }
