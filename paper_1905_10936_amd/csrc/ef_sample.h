@@ -24,22 +24,15 @@ struct SampleArgs {
     float *logp;
 };
 
-// 2^x for x <= 0 in 64 bits, to 1e-11 of it; 0 below 2^-60.
-__device__ __forceinline__ double power_of_two(double x)
+// 2^(j / POWERS) for the table that exponentials start from, by its series.
+constexpr int POWERS = 512;
+__device__ __forceinline__ double power(int j)
 {
-    const double r = __builtin_rint(x), f = (x - r) * 0.69314718055994530942;
-    double p = 1.0 / 3628800.0;
-    p = __builtin_fma(p, f, 1.0 / 362880.0);
-    p = __builtin_fma(p, f, 1.0 / 40320.0);
-    p = __builtin_fma(p, f, 1.0 / 5040.0);
-    p = __builtin_fma(p, f, 1.0 / 720.0);
-    p = __builtin_fma(p, f, 1.0 / 120.0);
-    p = __builtin_fma(p, f, 1.0 / 24.0);
-    p = __builtin_fma(p, f, 1.0 / 6.0);
-    p = __builtin_fma(p, f, 0.5);
-    p = __builtin_fma(p, f, 1.0);
-    p = __builtin_fma(p, f, 1.0);
-    return x >= -60.0 ? __builtin_amdgcn_ldexp(p, (int)r) : 0.0;
+    const double f = (double)j / POWERS * 0.69314718055994530942;
+    double p = 1.0;
+#pragma unroll
+    for (int k = 16; k >= 1; --k) p = __builtin_fma(p * f, 1.0 / k, 1.0);
+    return p;
 }
 
 // A value as a whole number of the same order; 0 and -0 are one.
@@ -50,37 +43,47 @@ __device__ __forceinline__ unsigned key_of(float v)
 }
 __device__ __forceinline__ float value_of(unsigned key) { return __uint_as_float(key & 0x80000000u ? key & 0x7fffffffu : ~key); }
 
-template <class V>
-__device__ __forceinline__ V from_lane(V v, int lane);
-template <>
-__device__ __forceinline__ unsigned from_lane(unsigned v, int lane) { return (unsigned)__builtin_amdgcn_ds_bpermute(lane * 4, (int)v); }
-template <>
-__device__ __forceinline__ double from_lane(double v, int lane)
+// What a lane gets of another one by a row's shift or broadcast; 0 where there is none.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ unsigned moved(unsigned v)
+{
+    return (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xf, false);
+}
+template <int CTRL, int ROWS>
+__device__ __forceinline__ double moved(double v)
 {
     const uint64_t b = (uint64_t)__double_as_longlong(v);
-    return __longlong_as_double((long long)((uint64_t)from_lane((unsigned)b, lane) | (uint64_t)from_lane((unsigned)(b >> 32), lane) << 32));
+    return __longlong_as_double((long long)((uint64_t)moved<CTRL, ROWS>((unsigned)b) | (uint64_t)moved<CTRL, ROWS>((unsigned)(b >> 32)) << 32));
 }
-// Sum over the lanes up to this one.
+// Sum over the lanes up to this one: within rows of 16, then a row's last lane to the rows behind it.
 template <class V>
-__device__ __forceinline__ V upto_lane(V v, int lane)
+__device__ __forceinline__ V upto_lane(V v)
 {
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-        const V other = from_lane(v, lane - d < 0 ? lane : lane - d);
-        if (lane >= d) v += other;
-    }
+    v += moved<0x111, 0xf>(v);
+    v += moved<0x112, 0xf>(v);
+    v += moved<0x114, 0xf>(v);
+    v += moved<0x118, 0xf>(v);
+    v += moved<0x142, 0xa>(v);
+    v += moved<0x143, 0xc>(v);
     return v;
+}
+__device__ __forceinline__ unsigned of_last_lane(unsigned v) { return (unsigned)__builtin_amdgcn_readlane((int)v, 63); }
+__device__ __forceinline__ double of_last_lane(double v)
+{
+    const uint64_t b = (uint64_t)__double_as_longlong(v);
+    return __longlong_as_double((long long)((uint64_t)of_last_lane((unsigned)b) | (uint64_t)of_last_lane((unsigned)(b >> 32)) << 32));
 }
 
 // LANES threads that have a row: a wavefront, or the whole workgroup.
 template <int LANES>
 struct Team {
     static constexpr int WAVES = LANES / 64, THREADS = LANES < 256 ? 256 : LANES, TEAMS = THREADS / LANES;
-    static constexpr int BINS = LANES == 64 ? 512 : 2048, LISTED = LANES == 64 ? 64 : 512;
+    static constexpr int BINS = LANES == 64 ? 512 : 2048, LISTED = LANES == 64 ? 64 : 256;
     struct Shared {
         double bins[BINS], wave_sum[WAVES], sorted_weight[LISTED], above;
         uint64_t list[LISTED], sorted[LISTED];
         int64_t place;
+        unsigned long long first;
         unsigned wave_count[WAVES], listed, least, most, bin, key, bad;
         float wave_top[WAVES];
     };
@@ -98,9 +101,9 @@ struct Team {
     static __device__ __forceinline__ double upto(double v, double *at, double &all)
     {
         const int lane = threadIdx.x % 64;
-        v = upto_lane(v, lane);
+        v = upto_lane(v);
         if constexpr (LANES == 64) {
-            all = from_lane(v, 63);
+            all = of_last_lane(v);
         } else {
             sync();
             if (lane == 63) at[threadIdx.x / 64] = v;
@@ -209,8 +212,36 @@ struct Sampler {
     float least;
     int64_t last;
 
-    __device__ __forceinline__ double weight(float v) const { return power_of_two(((double)v - (double)top) * factor); }
+    const double *powers;
+
+    // 2^x, x = (v - top) log2(e) / T: a table's power for x in steps of 1 / POWERS, what is left of x, at most 1 / 1024, by three terms in fp32 (1e-10 of the
+    // whole), the exponent added on.  Below 2^-60 all are that.
+    __device__ __forceinline__ double weight(float v) const
+    {
+        constexpr double STEPS = 1.5 * (double)(1ll << 52) / POWERS;
+        const double x = fmax(((double)v - (double)top) * factor, -60.0), steps = x + STEPS;
+        const int k = (int)(unsigned)(uint64_t)__double_as_longlong(steps);
+        const float f = (float)(x - (steps - STEPS));
+        const float e = f * __builtin_fmaf(f, __builtin_fmaf(f, 0.0555041087f, 0.240226507f), 0.693147181f);
+        const double from = powers[k & (POWERS - 1)], p = __builtin_fma(from, (double)e, from);
+        return __longlong_as_double((long long)((uint64_t)__double_as_longlong(p) + ((uint64_t)(int64_t)(k >> 9) << 52)));
+    }
     __device__ __forceinline__ double mass(float v) const { return (weight(v) + grid) - grid; }
+    // f(value, place, weight_of(value)) of everything kept; the weights of eight first, without a branch
+    template <class W, class F>
+    __device__ __forceinline__ void each_kept(W weight_of, F f) const
+    {
+        row.each([&](const Eight<T> &e, int64_t at) {
+            if (largest(e) >= least) {
+                double w[8];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) w[k] = weight_of(e[k]);
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    if (e[k] > least || (e[k] == least && at + k <= last)) f(e[k], at + k, w[k]);
+            }
+        });
+    }
     // f(value, place) of everything kept
     template <class F>
     __device__ __forceinline__ void each_kept(F f) const
@@ -275,8 +306,8 @@ struct Sampler {
         float low = least, high = top;
         for (int level = 0;; ++level) {
             clear_bins();
-            each_kept([&](float v, int64_t) {
-                if (v >= low && v <= high) unsafeAtomicAdd(&s.bins[bin_of(v, origin, scale)], weight_of(v));
+            each_kept(weight_of, [&](float v, int64_t, double w) {
+                if (v >= low && v <= high) unsafeAtomicAdd(&s.bins[bin_of(v, origin, scale)], w);
             });
             // from the second level on it is a bin that reaches the target which is taken apart
             if (!find_bin(above, [&](double all) { return level == 0 ? target_of(all) : target; }, target, level > 0)) return;
@@ -338,6 +369,19 @@ struct Sampler {
         last = s.place;
     }
 
+    // The first entry of the order alone.
+    __device__ __forceinline__ void first_alone()
+    {
+        least = top;
+        int64_t place = INT64_MAX;
+        each_kept([&](float, int64_t at) { place = place < at ? place : at; });
+        if (threadIdx.x % LANES == 0) s.first = ~0ull;
+        Of::sync();
+        if (place != INT64_MAX) atomicMin(&s.first, (unsigned long long)place);
+        Of::sync();
+        last = (int64_t)s.first;
+    }
+
     // The cut among `n` entries of one value, each of weight w.
     __device__ __forceinline__ void in_places(float value, unsigned n, double above, double target, double w)
     {
@@ -356,7 +400,7 @@ struct Sampler {
 #pragma unroll
             for (int k = 0; k < 8; ++k) mine += there(e, at, k);
         });
-        const unsigned sum = upto_lane(mine, lane);
+        const unsigned sum = upto_lane(mine);
         Of::sync();
         if (lane == 63) s.wave_count[wave] = sum;
         Of::sync();
@@ -368,14 +412,14 @@ struct Sampler {
                 unsigned here = 0;
 #pragma unroll
                 for (int k = 0; k < 8; ++k) here += there(e, at, k);
-                const unsigned upto = upto_lane(here, lane);
+                const unsigned upto = upto_lane(here);
                 unsigned c = before + upto - here;
                 if (c < rank && before + upto >= rank) {
 #pragma unroll
                     for (int k = 0; k < 8; ++k)
                         if (there(e, at, k) && ++c == rank) s.place = at + k;
                 }
-                before += from_lane(upto, 63);
+                before += of_last_lane(upto);
             });
         }
         Of::sync();
@@ -406,6 +450,9 @@ __global__ __launch_bounds__(Team<LANES>::THREADS) void k_sample(SampleArgs a)
 {
     using Of = Team<LANES>;
     __shared__ typename Of::Shared shared[Of::TEAMS];
+    __shared__ double powers[POWERS];
+    for (int i = threadIdx.x; i < POWERS; i += Of::THREADS) powers[i] = power(i);
+    __syncthreads();
     const int lane = threadIdx.x % 64, wave = threadIdx.x % LANES / 64;
     const int64_t row = a.first + (int64_t)blockIdx.x * Of::TEAMS + (Of::TEAMS > 1 ? threadIdx.x / LANES : 0);
     if (row >= a.rows) return;          // whole wavefronts, which meet no other
@@ -446,6 +493,7 @@ __global__ __launch_bounds__(Team<LANES>::THREADS) void k_sample(SampleArgs a)
         return;
     }
     r.top = top;
+    r.powers = powers;
     r.least = -3.402823466e38f;
     r.last = INT64_MAX;
     // The sum of the row's masses stays below 2^52 times their grid.
@@ -466,13 +514,14 @@ __global__ __launch_bounds__(Team<LANES>::THREADS) void k_sample(SampleArgs a)
 
     // ---- what is kept
     const bool greedy = heat == 0.0f || top_p <= 0.0f;
-    const int64_t k = greedy ? 1 : top_k;
-    r.factor = greedy ? 0.0 : 1.4426950408889634074 / (double)heat;
-    if (k > 0 && k < a.vocab) {
-        r.leave_out(k, mine);
-        r.cut(24.0, [](float) { return 1.0; }, [&](double) { return (double)k; });
+    r.factor = heat == 0.0f ? 1.0 : 1.4426950408889634074 / (double)heat;
+    if (greedy || top_k == 1) {
+        r.first_alone();
+    } else if (top_k > 0 && top_k < a.vocab) {
+        r.leave_out(top_k, mine);
+        r.cut(24.0, [](float) { return 1.0; }, [&](double) { return (double)top_k; });
     }
-    if (!greedy && top_p < 1.0f)
+    if (!greedy && top_k != 1 && top_p < 1.0f)
         r.cut(fmin(24.0 * (double)heat, 1e30), [&](float v) { return r.mass(v); }, [&](double all) { return (double)top_p * all; });
     const double floor_p = fmin((double)min_p, 1.0);
     const auto kept_mass = [&](float v) {
@@ -482,8 +531,8 @@ __global__ __launch_bounds__(Team<LANES>::THREADS) void k_sample(SampleArgs a)
 
     // ---- the draw: the first entry with more than u of the kept mass up to it
     double own = 0.0;
-    r.each_kept([&](float v, int64_t) { own += kept_mass(v); });
-    const double upto = upto_lane(own, lane);
+    r.each_kept(kept_mass, [&](float, int64_t, double m) { own += m; });
+    const double upto = upto_lane(own);
     double total = 0.0, before = 0.0;
     if constexpr (LANES > 64) {
         Of::sync();
@@ -492,7 +541,7 @@ __global__ __launch_bounds__(Team<LANES>::THREADS) void k_sample(SampleArgs a)
 #pragma unroll
         for (int i = 0; i < Of::WAVES; ++i) total += s.wave_sum[i];
     } else {
-        total = from_lane(upto, 63);
+        total = of_last_lane(upto);
     }
     const double target = (double)u * total;
     if constexpr (LANES > 64) {
@@ -508,7 +557,7 @@ __global__ __launch_bounds__(Team<LANES>::THREADS) void k_sample(SampleArgs a)
             m[k] = e[k] > r.least || (e[k] == r.least && at + k <= r.last) ? kept_mass(e[k]) : 0.0;
             here += m[k];
         }
-        const double sum = upto_lane(here, lane);
+        const double sum = upto_lane(here);
         double c = before + (sum - here);
         if (c <= target && before + sum > target) {
 #pragma unroll
@@ -520,7 +569,7 @@ __global__ __launch_bounds__(Team<LANES>::THREADS) void k_sample(SampleArgs a)
                 c += m[k];
             }
         }
-        before += from_lane(sum, 63);
+        before += of_last_lane(sum);
     });
 }
 
