@@ -80,11 +80,9 @@ struct Team {
     static constexpr int WAVES = LANES / 64, THREADS = LANES < 256 ? 256 : LANES, TEAMS = THREADS / LANES;
     static constexpr int BINS = LANES == 64 ? 512 : 2048, LISTED = LANES == 64 ? 64 : 256;
     struct Shared {
-        double bins[BINS], wave_sum[WAVES], sorted_weight[LISTED], above;
+        double bins[BINS], wave_sum[WAVES], sorted_weight[LISTED], above;      // bins of numbers of entries: words in the same place
         uint64_t list[LISTED], sorted[LISTED];
-        int64_t place;
-        unsigned long long first;
-        unsigned wave_count[WAVES], listed, least, most, bin, key, bad;
+        unsigned wave_count[WAVES], listed, least, most, bin, key, place;
         float wave_top[WAVES];
     };
     static __device__ __forceinline__ void sync()
@@ -151,7 +149,7 @@ struct SampleRow {
                     e.lo = p[0];
                     e.hi = p[1];
                 }
-                f(e, (int64_t)at);
+                f(e, (unsigned)at);
             }
         } else {
             from_memory(f);
@@ -170,7 +168,7 @@ struct SampleRow {
             }
 #pragma unroll
             for (int k = 0; k < AHEAD; ++k)
-                if (i + k * 512 < end) f(e[k], i + k * 512 + threadIdx.x % 64 * 8);
+                if (i + k * 512 < end) f(e[k], (unsigned)(i + k * 512) + threadIdx.x % 64 * 8);
         }
     }
     __device__ __forceinline__ SampleRow(const T *row, T *buffer, int64_t n)
@@ -186,7 +184,7 @@ struct SampleRow {
     template <class F>
     __device__ __forceinline__ void load(F f)
     {
-        from_memory([&](const Eight<T> &e, int64_t at) {
+        from_memory([&](const Eight<T> &e, unsigned at) {
             if constexpr (HELD) {
                 u32x4 *p = reinterpret_cast<u32x4 *>(held + at);
                 if constexpr (sizeof(T) == 2) {
@@ -206,13 +204,12 @@ struct Sampler {
     using Of = Team<LANES>;
     typename Of::Shared &s;
     SampleRow<T, LANES, HELD> row;
+    const double *powers;
     float top;
     double factor, grid;        // log2(e) / T; what makes (w + grid) - grid a multiple of a power of two
     // kept: larger than `least`, or equal to it and at most at `last`
     float least;
-    int64_t last;
-
-    const double *powers;
+    unsigned last;
 
     // 2^x, x = (v - top) log2(e) / T: a table's power for x in steps of 1 / POWERS, what is left of x, at most 1 / 1024, by three terms in fp32 (1e-10 of the
     // whole), the exponent added on.  Below 2^-60 all are that.
@@ -227,36 +224,45 @@ struct Sampler {
         return __longlong_as_double((long long)((uint64_t)__double_as_longlong(p) + ((uint64_t)(int64_t)(k >> 9) << 52)));
     }
     __device__ __forceinline__ double mass(float v) const { return (weight(v) + grid) - grid; }
-    // f(value, place, weight_of(value)) of everything kept; the weights of eight first, without a branch
-    template <class W, class F>
-    __device__ __forceinline__ void each_kept(W weight_of, F f) const
-    {
-        row.each([&](const Eight<T> &e, int64_t at) {
-            if (largest(e) >= least) {
-                double w[8];
-#pragma unroll
-                for (int k = 0; k < 8; ++k) w[k] = weight_of(e[k]);
-#pragma unroll
-                for (int k = 0; k < 8; ++k)
-                    if (e[k] > least || (e[k] == least && at + k <= last)) f(e[k], at + k, w[k]);
-            }
-        });
-    }
-    // f(value, place) of everything kept
+
+    // f(eight values, place of the first) for the eights that hold something kept, -inf in the place of what is not.
     template <class F>
     __device__ __forceinline__ void each_kept(F f) const
     {
-        row.each([&](const Eight<T> &e, int64_t at) {
-            if (largest(e) >= least) {
+        const float above = value_of(key_of(least) + 1);
+        row.each([&](const Eight<T> &e, unsigned at) {
+            // one comparison to an entry: all of them at most at `last`, or (but for the one eight that has it) behind
+            const float from = at + 7 <= last ? least : above;
+            float v[8], most = -INFINITY;
 #pragma unroll
-                for (int k = 0; k < 8; ++k)
-                    if (e[k] > least || (e[k] == least && at + k <= last)) f(e[k], at + k);
+            for (int k = 0; k < 8; ++k) {
+                v[k] = e[k] >= from ? e[k] : -INFINITY;
+                most = fmaxf(most, v[k]);
             }
+            if (last - at < 7) {
+#pragma unroll
+                for (int k = 0; k < 7; ++k)
+                    if (at + k <= last && e[k] == least) v[k] = most = e[k];
+            }
+            if (most > -INFINITY) f(v, at);
         });
     }
-    static __device__ __forceinline__ int bin_of(float v, double origin, double scale)
+
+    // A bin's number for a value: linear, from 0 for `origin` on, the last for all that is far.  `unit`: a power of two that keeps differences in fp32's range.
+    struct Scale {
+        float unit, origin, factor;
+        __device__ __forceinline__ int bin(float v) const
+        {
+            return (int)fminf(__builtin_fmaf(v, -unit, origin) * factor, (float)(Of::BINS - 1));
+        }
+    };
+    static __device__ __forceinline__ Scale scale_of(float origin, double range)
     {
-        return (int)fmin((origin - (double)v) * scale, (double)(Of::BINS - 1));
+        Scale x;
+        x.unit = range > 1e30 || fabsf(origin) > 1e37f ? 0x1p-20f : range < 1e-30 ? 0x1p100f : 1.0f;
+        x.origin = origin * x.unit;
+        x.factor = (float)fmin(Of::BINS / (range * (double)x.unit), 1e30);
+        return x;
     }
     __device__ __forceinline__ void clear_bins()
     {
@@ -269,9 +275,36 @@ struct Sampler {
         }
         Of::sync();
     }
+    template <bool COUNT>
+    __device__ __forceinline__ void add(int bin, double w)
+    {
+        if constexpr (COUNT)
+            atomicAdd(reinterpret_cast<unsigned *>(s.bins) + bin, 1u);
+        else
+            unsafeAtomicAdd(&s.bins[bin], w);
+    }
+    // One entry more in the list, if it has room, and in any case in `listed`.
+    __device__ __forceinline__ void list(float v, unsigned place)
+    {
+        const unsigned long long here = __ballot(1);
+        const int lane = threadIdx.x % 64, leader = __builtin_ctzll(here);
+        unsigned n = 0;
+        if (lane == leader) n = atomicAdd(&s.listed, (unsigned)__builtin_popcountll(here));
+        n = (unsigned)__builtin_amdgcn_readlane((int)n, leader) + (unsigned)__builtin_popcountll(here & ((1ull << lane) - 1));
+        if (n < Of::LISTED) s.list[n] = (uint64_t)~key_of(v) << 32 | (uint64_t)place;
+    }
+    // Where entry i of the list stands among its n.
+    __device__ __forceinline__ int rank(int i, int n) const
+    {
+        const uint64_t mine = s.list[i];
+        int rank = 0;
+#pragma unroll 8
+        for (int j = 0; j < n; ++j) rank += s.list[j] < mine;
+        return rank;
+    }
     // The bin in which the sums from the first one on reach the target, which `target_of` makes of the sum of all of them: s.bin, and in s.above `above` with
     // all bins before it.  Returns false where the target is not below that sum, unless it is known to be reached.
-    template <class F>
+    template <bool COUNT, class F>
     __device__ __forceinline__ bool find_bin(double above, F target_of, double &target, bool reached = false)
     {
         constexpr int PER = Of::BINS / LANES;
@@ -280,7 +313,7 @@ struct Sampler {
         double own[PER], sum = 0.0, all;
 #pragma unroll
         for (int k = 0; k < PER; ++k) {
-            own[k] = s.bins[first + k];
+            own[k] = COUNT ? (double)reinterpret_cast<const unsigned *>(s.bins)[first + k] : s.bins[first + k];
             sum += own[k];
         }
         double before = Of::upto(sum, s.wave_sum, all) - sum + above;
@@ -298,62 +331,70 @@ struct Sampler {
         return true;
     }
 
-    // Keeps, of what is kept, the beginning whose weights reach a target: all entries before which there is less.
-    template <class W, class F>
-    __device__ __forceinline__ void cut(double range, W weight_of, F target_of)
+    // Keeps, of what is kept, the beginning whose weights (COUNT: of one each) reach a target: all entries before which there is less.
+    template <bool COUNT, class F>
+    __device__ __forceinline__ void cut(double range, F target_of)
     {
-        double origin = top, scale = Of::BINS / range, above = 0.0, target = 0.0;
-        float low = least, high = top;
+        double above = 0.0, target = 0.0;
+        float low = -3.402823466e38f, high = top;
+        Scale x = scale_of(top, range);
         for (int level = 0;; ++level) {
             clear_bins();
-            each_kept(weight_of, [&](float v, int64_t, double w) {
-                if (v >= low && v <= high) unsafeAtomicAdd(&s.bins[bin_of(v, origin, scale)], w);
+            each_kept([&](const float *v, unsigned) {
+                double w[8];
+                if constexpr (!COUNT) {
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) w[k] = mass(v[k]);
+                }
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    if (v[k] >= low && v[k] <= high) add<COUNT>(x.bin(v[k]), w[k]);
             });
             // from the second level on it is a bin that reaches the target which is taken apart
-            if (!find_bin(above, [&](double all) { return level == 0 ? target_of(all) : target; }, target, level > 0)) return;
+            if (!find_bin<COUNT>(above, [&](double all) { return level == 0 ? target_of(all) : target; }, target, level > 0)) return;
             above = s.above;
             const int bin = (int)s.bin;
-            each_kept([&](float v, int64_t at) {
-                if (v >= low && v <= high && bin_of(v, origin, scale) == bin) {
-                    const unsigned key = key_of(v);
-                    const unsigned long long here = __ballot(1);
-                    const int lane = threadIdx.x % 64, leader = __builtin_ctzll(here);
-                    unsigned n = 0;
-                    if (lane == leader) n = atomicAdd(&s.listed, (unsigned)__builtin_popcountll(here));
-                    n = (unsigned)__builtin_amdgcn_readlane((int)n, leader) + (unsigned)__builtin_popcountll(here & ((1ull << lane) - 1));
-                    if (n < Of::LISTED) s.list[n] = (uint64_t)~key << 32 | (uint64_t)(unsigned)at;
-                    atomicMin(&s.least, key);
-                    atomicMax(&s.most, key);
+            each_kept([&](const float *v, unsigned at) {
+                unsigned those = 0;
+#pragma unroll
+                for (int k = 0; k < 8; ++k) those |= v[k] >= low && v[k] <= high && x.bin(v[k]) == bin ? 1u << k : 0u;
+                if (those) {
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) {
+                        if (those >> k & 1) {
+                            list(v[k], at + k);
+                            atomicMin(&s.least, key_of(v[k]));
+                            atomicMax(&s.most, key_of(v[k]));
+                        }
+                    }
                 }
             });
             Of::sync();
             const unsigned listed = s.listed, lo = s.least, hi = s.most;
             if (listed <= Of::LISTED) {
-                in_list((int)listed, above, target, weight_of);
+                in_list<COUNT>((int)listed, above, target);
                 return;
             }
             low = value_of(lo);
             high = value_of(hi);
             if (lo == hi) {
-                in_places(low, listed, above, target, weight_of(low));
+                in_places(low, listed, above, target, COUNT ? 1.0 : mass(low));
                 return;
             }
-            origin = high;
-            scale = Of::BINS / ((double)high - (double)low);
+            x = scale_of(high, (double)high - (double)low);
         }
     }
 
     // The cut within the listed entries: each finds its rank among them, and the sum of weights up to it.
-    template <class W>
-    __device__ __forceinline__ void in_list(int n, double above, double target, W weight_of)
+    template <bool COUNT>
+    __device__ __forceinline__ void in_list(int n, double above, double target)
     {
         const int i = threadIdx.x % LANES;
         if (i < n) {
             const uint64_t mine = s.list[i];
-            int rank = 0;
-            for (int j = 0; j < n; ++j) rank += s.list[j] < mine;
-            s.sorted[rank] = mine;
-            s.sorted_weight[rank] = weight_of(value_of(~(unsigned)(mine >> 32)));
+            const int at = rank(i, n);
+            s.sorted[at] = mine;
+            s.sorted_weight[at] = COUNT ? 1.0 : mass(value_of(~(unsigned)(mine >> 32)));
         }
         Of::sync();
         const double w = i < n ? s.sorted_weight[i] : 0.0;
@@ -362,7 +403,7 @@ struct Sampler {
         // the last one before which there is less than the target; the first of the bin is one
         if (i < n && before < target && (i == n - 1 || sum >= target)) {
             s.key = ~(unsigned)(s.sorted[i] >> 32);
-            s.place = (int64_t)(unsigned)s.sorted[i];
+            s.place = (unsigned)s.sorted[i];
         }
         Of::sync();
         least = value_of(s.key);
@@ -373,13 +414,18 @@ struct Sampler {
     __device__ __forceinline__ void first_alone()
     {
         least = top;
-        int64_t place = INT64_MAX;
-        each_kept([&](float, int64_t at) { place = place < at ? place : at; });
-        if (threadIdx.x % LANES == 0) s.first = ~0ull;
+        unsigned place = 0xffffffffu;
+        each_kept([&](const float *v, unsigned at) {
+#pragma unroll
+            for (int k = 7; k >= 0; --k)
+                if (v[k] > -INFINITY) place = min(place, at + k);
+        });
         Of::sync();
-        if (place != INT64_MAX) atomicMin(&s.first, (unsigned long long)place);
+        if (threadIdx.x % LANES == 0) s.place = 0xffffffffu;
         Of::sync();
-        last = (int64_t)s.first;
+        if (place != 0xffffffffu) atomicMin(&s.place, place);
+        Of::sync();
+        last = s.place;
     }
 
     // The cut among `n` entries of one value, each of weight w.
@@ -391,12 +437,11 @@ struct Sampler {
         while (j > 1.0 && above + (j - 1.0) * w >= target) j -= 1.0;
         const unsigned rank = (unsigned)fmax(j, 1.0);
         const int lane = threadIdx.x % 64, wave = threadIdx.x % LANES / 64;
-        const float was_least = least;
-        const int64_t was_last = last;
         // those already cut off stand behind all that are kept
-        const auto there = [&](const Eight<T> &e, int64_t at, int k) { return e[k] == value && (value > was_least || at + k <= was_last); };
+        const unsigned until = value > least ? 0xffffffffu : last;
+        const auto there = [&](const Eight<T> &e, unsigned at, int k) { return e[k] == value && at + k <= until; };
         unsigned mine = 0;
-        row.each([&](const Eight<T> &e, int64_t at) {
+        row.each([&](const Eight<T> &e, unsigned at) {
 #pragma unroll
             for (int k = 0; k < 8; ++k) mine += there(e, at, k);
         });
@@ -408,7 +453,7 @@ struct Sampler {
         int in = 0;
         while (in < Of::WAVES - 1 && before + s.wave_count[in] < rank) before += s.wave_count[in++];
         if (wave == in) {
-            row.each([&](const Eight<T> &e, int64_t at) {
+            row.each([&](const Eight<T> &e, unsigned at) {
                 unsigned here = 0;
 #pragma unroll
                 for (int k = 0; k < 8; ++k) here += there(e, at, k);
@@ -427,21 +472,80 @@ struct Sampler {
         last = s.place;
     }
 
-    // Of few entries all but about those are left out at once: k threads' largest values are k entries, so that what is below the least of them cannot be among
-    // the first k.
+    // Of few entries all but about those are left out at once: k values from different places (`mine`: a thread's largest; else the eights' largest) are k
+    // entries, so that what is below the least of them is not among the first k.
     __device__ __forceinline__ void leave_out(int64_t k, float mine)
     {
-        if (k > LANES / 2) return;
-        const double origin = top, scale = Of::BINS / 24.0;
+        const bool few = k <= LANES / 2;
+        if (!few && k * 16 > row.vocab) return;
+        const Scale x = scale_of(top, 24.0);
+        const auto each = [&](auto f) {
+            if (few) {
+                if (mine > -INFINITY) f(mine);
+            } else {
+                row.each([&](const Eight<T> &e, unsigned) {
+                    const float most = largest(e);
+                    if (most > -INFINITY) f(most);
+                });
+            }
+        };
         clear_bins();
-        const bool some = mine >= least;
-        const int bin = some ? bin_of(mine, origin, scale) : Of::BINS;
-        if (some) unsafeAtomicAdd(&s.bins[bin], 1.0);
+        each([&](float v) { add<true>(x.bin(v), 1.0); });
         double target;
-        if (!find_bin(0.0, [&](double) { return (double)k; }, target)) return;
-        if (bin <= (int)s.bin) atomicMin(&s.least, key_of(mine));
+        if (!find_bin<true>(0.0, [&](double) { return (double)k; }, target)) return;
+        const int bin = (int)s.bin;
+        float lowest = INFINITY;
+        each([&](float v) {
+            if (x.bin(v) <= bin) lowest = fminf(lowest, v);
+        });
+        lowest = -over_lanes<Max, 64>(-lowest);
+        if (threadIdx.x % 64 == 0 && lowest < INFINITY) atomicMin(&s.least, key_of(lowest));
         Of::sync();
         least = value_of(s.least);
+    }
+
+    // Draws among at most k entries, all of which the list holds: every filter and the draw within it.  False: it does not hold them.
+    __device__ __forceinline__ bool draw_listed(int k, double top_p, double floor_p, double u, unsigned &token, float &value)
+    {
+        each_kept([&](const float *v, unsigned at) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (v[i] > -INFINITY) list(v[i], at + i);
+        });
+        Of::sync();
+        const int n = (int)s.listed, i = threadIdx.x % LANES;
+        if (n > Of::LISTED) return false;
+        const uint64_t mine = i < n ? s.list[i] : 0;
+        const int order = i < n ? rank(i, n) : 0;
+        const float v = value_of(~(unsigned)(mine >> 32));
+        const double w = i < n && order < k ? weight(v) : 0.0;
+        if (i < n) s.sorted_weight[order] = (w + grid) - grid;
+        Of::sync();
+        // the mass of the first k, and before each
+        const double m = i < n ? s.sorted_weight[i] : 0.0;
+        double all;
+        const double upto = Of::upto(m, s.wave_sum, all);
+        if (i < n) s.bins[i] = upto - m;
+        Of::sync();
+        const bool kept = i < n && order < k && (order == 0 || (s.bins[order] < top_p * all && w >= floor_p));
+        const double mass = kept ? (w + grid) - grid : 0.0;
+        if (i < n) {
+            s.sorted[i] = mine & 0xffffffffu;
+            s.sorted_weight[i] = mass;
+        }
+        Of::sync();
+        double before = 0.0, total = 0.0;
+        if (kept) {
+#pragma unroll 4
+            for (int j = 0; j < n; ++j) {
+                const double other = s.sorted_weight[j];
+                total += other;
+                before += s.sorted[j] < (mine & 0xffffffffu) ? other : 0.0;
+            }
+        }
+        token = kept && before <= u * total && before + mass > u * total ? (unsigned)mine : 0xffffffffu;       // one thread's
+        value = v;
+        return true;
     }
 };
 
@@ -466,7 +570,7 @@ __global__ __launch_bounds__(Team<LANES>::THREADS) void k_sample(SampleArgs a)
     // ---- the largest value; what is no distribution
     float mine = -INFINITY;
     bool bad = false;
-    r.row.load([&](const Eight<T> &e, int64_t) {
+    r.row.load([&](const Eight<T> &e, unsigned) {
         mine = fmaxf(mine, largest(e));
 #pragma unroll
         for (int k = 0; k < 8; ++k) bad = bad || e[k] != e[k];
@@ -495,13 +599,13 @@ __global__ __launch_bounds__(Team<LANES>::THREADS) void k_sample(SampleArgs a)
     r.top = top;
     r.powers = powers;
     r.least = -3.402823466e38f;
-    r.last = INT64_MAX;
+    r.last = 0xffffffffu;
     // The sum of the row's masses stays below 2^52 times their grid.
     r.grid = __builtin_amdgcn_ldexp(1.5, 64 - __builtin_clzll((unsigned long long)a.vocab));
     // The policy's own sum, in fp32's exponentials: a term's error is its own, and the sums are in 64 bits.
     double whole = 0.0;
     if (a.logp) {
-        r.row.each([&](const Eight<T> &e, int64_t) {
+        r.row.each([&](const Eight<T> &e, unsigned) {
             float v[8];
 #pragma unroll
             for (int k = 0; k < 8; ++k) v[k] = __builtin_amdgcn_exp2f((e[k] - top) * 1.44269504f);
@@ -514,15 +618,32 @@ __global__ __launch_bounds__(Team<LANES>::THREADS) void k_sample(SampleArgs a)
 
     // ---- what is kept
     const bool greedy = heat == 0.0f || top_p <= 0.0f;
-    r.factor = heat == 0.0f ? 1.0 : 1.4426950408889634074 / (double)heat;
     if (greedy || top_k == 1) {
         r.first_alone();
-    } else if (top_k > 0 && top_k < a.vocab) {
-        r.leave_out(top_k, mine);
-        r.cut(24.0, [](float) { return 1.0; }, [&](double) { return (double)top_k; });
+        if (threadIdx.x % LANES == 0) {
+            a.tokens[row] = (int64_t)r.last;
+            if (a.logp) a.logp[row] = (float)-log(whole);
+        }
+        return;
     }
-    if (!greedy && top_k != 1 && top_p < 1.0f)
-        r.cut(fmin(24.0 * (double)heat, 1e30), [&](float v) { return r.mass(v); }, [&](double all) { return (double)top_p * all; });
+    r.factor = 1.4426950408889634074 / (double)heat;
+    if (top_k > 0 && top_k < a.vocab) {
+        r.leave_out(top_k, mine);
+        if (top_k <= Of::LISTED / 2) {
+            unsigned token;
+            float value;
+            if (r.draw_listed((int)top_k, (double)top_p, fmin((double)min_p, 1.0), (double)u, token, value)) {
+                if (token != 0xffffffffu) {
+                    a.tokens[row] = (int64_t)token;
+                    if (a.logp) a.logp[row] = (float)(((double)value - (double)top) - log(whole));
+                }
+                return;
+            }
+        }
+        r.template cut<true>(24.0, [&](double) { return (double)top_k; });
+    }
+    if (top_p < 1.0f)
+        r.template cut<false>(24.0 * (double)heat, [&](double all) { return (double)top_p * all; });
     const double floor_p = fmin((double)min_p, 1.0);
     const auto kept_mass = [&](float v) {
         const double w = r.weight(v);
@@ -531,7 +652,23 @@ __global__ __launch_bounds__(Team<LANES>::THREADS) void k_sample(SampleArgs a)
 
     // ---- the draw: the first entry with more than u of the kept mass up to it
     double own = 0.0;
-    r.each_kept(kept_mass, [&](float, int64_t, double m) { own += m; });
+    const auto sum_of = [&](const double *m) { return ((m[0] + m[1]) + (m[2] + m[3])) + ((m[4] + m[5]) + (m[6] + m[7])); };
+    if (r.last == 0xffffffffu && r.least == -3.402823466e38f && floor_p <= 0.0) {
+        // nothing is left out: -inf has no mass by itself
+        r.row.each([&](const Eight<T> &e, unsigned) {
+            double m[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) m[k] = r.mass(e[k]);
+            own += sum_of(m);
+        });
+    } else {
+        r.each_kept([&](const float *v, unsigned) {
+            double m[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) m[k] = kept_mass(v[k]);
+            own += sum_of(m);
+        });
+    }
     const double upto = upto_lane(own);
     double total = 0.0, before = 0.0;
     if constexpr (LANES > 64) {
@@ -549,12 +686,14 @@ __global__ __launch_bounds__(Team<LANES>::THREADS) void k_sample(SampleArgs a)
         while (in < Of::WAVES - 1 && before + s.wave_sum[in] <= target) before += s.wave_sum[in++];
         if (wave != in) return;
     }
-    r.row.each([&](const Eight<T> &e, int64_t at) {
+    // every eight of the wavefront, those with nothing kept too: the sums are the whole wavefront's
+    const float above = value_of(key_of(r.least) + 1);
+    r.row.each([&](const Eight<T> &e, unsigned at) {
         if (!__any(largest(e) >= r.least)) return;
         double m[8], here = 0.0;
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
-            m[k] = e[k] > r.least || (e[k] == r.least && at + k <= r.last) ? kept_mass(e[k]) : 0.0;
+            m[k] = kept_mass(e[k] >= (at + k <= r.last ? r.least : above) ? e[k] : -INFINITY);
             here += m[k];
         }
         const double sum = upto_lane(here);
@@ -563,7 +702,7 @@ __global__ __launch_bounds__(Team<LANES>::THREADS) void k_sample(SampleArgs a)
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
                 if (c <= target && c + m[k] > target) {
-                    a.tokens[row] = at + k;
+                    a.tokens[row] = (int64_t)(at + k);
                     if (a.logp) a.logp[row] = (float)(((double)e[k] - (double)top) - log(whole));
                 }
                 c += m[k];
