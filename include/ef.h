@@ -613,8 +613,8 @@ int ef_sample_tokens(ef_workspace *workspace, int64_t rows, int64_t vocab, int t
  *   flat      out   float[n_workers][flat_stride] (flat_stride >= the sizes' sum; not used with one worker), what lies behind a row's sum
  *                   is left as it is; or NULL: the tensors are scaled where they are
  *   norm      out   float[n_workers]
- * n_workers >= 1, 0 <= n_tensors <= 2^20; sizes up to 2^50 elements in all (EF_ERR_SIZE beyond, as for more workers than the workspace has
- * room for, which is above 4000).  What is written may share memory with nothing else of the call (EF_ERR_ARG): in place, every tensor is there once.
+ * n_workers >= 1, 0 <= n_tensors <= 2^20; sizes up to 2^50 elements in all (EF_ERR_SIZE beyond, as for more than the workspace has room for:
+ * n_tensors * (n_workers + 1) + 2048 * n_workers up to 2^23 always fits).  What is written may share memory with nothing else of the call (EF_ERR_ARG): in place, every tensor is there once.
  */
 int ef_grad_clip(ef_workspace *workspace, int n_workers, int64_t n_tensors, void *const *grads, const int64_t *sizes, const int *types,
                  float max_norm, float *flat, int64_t flat_stride, float *norm, void *stream);

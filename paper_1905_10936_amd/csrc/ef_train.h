@@ -243,56 +243,48 @@ try {
         if (!next) entries.push_back({place, i});
         before = i;
     }
-    const int64_t n = (int64_t)entries.size();
-    // Launches: all tensors of as many workers as fit a kernel's arguments, or a part of one worker's.
-    const int64_t each = std::min<int64_t>(std::max<int64_t>(n, 1), ef::CLIP_TENSORS), ranges = n ? ceil_div(n, each) : 1;
-    const int64_t workers = std::min<int64_t>(n_workers, ef::CLIP_TENSORS / each);
-    struct Range { int64_t first, last, base, length, chunk; int chunks, slot; };
-    std::vector<Range> all;
-    int64_t slots = 0;
-    for (int64_t r = 0; r < ranges; ++r) {
-        Range x{r * each, std::min(n, (r + 1) * each), 0, 0, 0, 0, (int)slots};
-        x.base = n ? entries[(size_t)x.first].place : 0;
-        x.length = (x.last < n ? entries[(size_t)x.last].place : total) - x.base;
-        x.chunk = std::max<int64_t>(ef::CLIP_LEAST, ceil_div(ceil_div(total, ef::CLIP_CHUNKS), ef::CLIP_LEAST) * ef::CLIP_LEAST);
-        x.chunks = (int)std::max<int64_t>(1, ceil_div(x.length, x.chunk));
-        slots += x.chunks;
-        all.push_back(x);
-    }
-    if (slots * n_workers > PART_FLOATS / 2) return EF_ERR_SIZE;
+    const int64_t n = (int64_t)entries.size(), words = n * (n_workers + 1), count = std::max<int64_t>(1, total);
     ef::ClipArgs a;
-    a.slots = (int)slots;
+    a.length = total;
+    // Chunks of 2048 to 16384 places; workgroups for 4096 in all, or 2048 for a worker.
+    a.chunk = std::min<int64_t>(ef::CLIP_MOST, ceil_div(count, (int64_t)ef::CLIP_GROUPS * ef::CLIP_LEAST) * ef::CLIP_LEAST);
+    const int64_t groups = std::min<int64_t>(ceil_div(count, a.chunk), std::max<int64_t>(256, std::min<int64_t>(ef::CLIP_GROUPS, 2 * ef::CLIP_GROUPS / n_workers)));
+    if (words + groups * n_workers > PART_FLOATS / 2 || words > 0x7fffffff || n_workers > 0xffff) return EF_ERR_SIZE;
+    a.tensors = (int)n;
     a.sums = reinterpret_cast<double *>(workspace->parts);
     a.flat = flat;
     a.flat_stride = n_workers > 1 ? flat_stride : 0;
+    a.norm = norm;
     a.max_norm = max_norm;
+    const auto word = [&](int64_t i) {
+        if (i < n) return (uint64_t)entries[(size_t)i].place;
+        const int64_t tensor = entries[(size_t)(i % n)].tensor;
+        return reinterpret_cast<uint64_t>(grads[(i / n - 1) * n_tensors + tensor]) | (types[tensor] == EF_TYPE_FP32 ? 1 : 0);
+    };
     const hipStream_t s = static_cast<hipStream_t>(stream);
-    for (int pass = 0; pass < 2; ++pass) {
-        for (int w = 0; w < n_workers; w += (int)workers) {
-            const int here = std::min<int>((int)workers, n_workers - w);
-            for (const Range &x : all) {
-                a.base = x.base;
-                a.length = x.length;
-                a.chunk = x.chunk;
-                a.tensors = (int)(x.last - x.first);
-                a.slot = x.slot;
-                a.worker = w;
-                a.norm = x.slot == 0 ? norm : nullptr;
-                for (int64_t i = x.first; i < x.last; ++i) {
-                    a.first[i - x.first] = entries[(size_t)i].place - x.base;
-                    for (int k = 0; k < here; ++k)
-                        a.at[k * a.tensors + (i - x.first)] = reinterpret_cast<uint64_t>(grads[(int64_t)(w + k) * n_tensors + entries[(size_t)i].tensor]) |
-                                                              (types[entries[(size_t)i].tensor] == EF_TYPE_FP32 ? 1 : 0);
-                }
-                const dim3 grid((unsigned)x.chunks, (unsigned)here);
-                if (pass == 0)
-                    hipLaunchKernelGGL(ef::k_clip_norm, grid, dim3(ef::CLIP_THREADS), 0, s, a);
-                else
-                    hipLaunchKernelGGL(ef::k_clip_scale, grid, dim3(ef::CLIP_THREADS), 0, s, a);
-                EF_HIP(hipGetLastError());
-            }
+    const dim3 grid((unsigned)groups, (unsigned)n_workers), threads(ef::CLIP_THREADS);
+    if (words <= ef::CLIP_WORDS) {
+        ef::ClipDirect d;
+        d.a = a;
+        for (int64_t i = 0; i < words; ++i) d.words[i] = word(i);
+        hipLaunchKernelGGL(ef::k_clip_norm<ef::ClipDirect>, grid, threads, 0, s, d);
+        hipLaunchKernelGGL(ef::k_clip_scale<ef::ClipDirect>, grid, threads, 0, s, d);
+    } else {
+        ef::ClipListed l;
+        l.a = a;
+        uint64_t *const to = reinterpret_cast<uint64_t *>(workspace->parts) + groups * n_workers;
+        l.words = to;
+        for (int64_t i = 0; i < words; i += ef::CLIP_WORDS) {
+            ef::ClipWords w;
+            w.to = to + i;
+            w.n = (int)std::min<int64_t>(ef::CLIP_WORDS, words - i);
+            for (int k = 0; k < w.n; ++k) w.words[k] = word(i + k);
+            hipLaunchKernelGGL(ef::k_clip_words, dim3(1), dim3(ef::CLIP_WORDS), 0, s, w);
         }
+        hipLaunchKernelGGL(ef::k_clip_norm<ef::ClipListed>, grid, threads, 0, s, l);
+        hipLaunchKernelGGL(ef::k_clip_scale<ef::ClipListed>, grid, threads, 0, s, l);
     }
+    EF_HIP(hipGetLastError());
     return EF_OK;
 } catch (const std::bad_alloc &) {
     return EF_ERR_SIZE;
