@@ -47,8 +47,17 @@ __device__ __forceinline__ float2 sigmoid(float a, int gate)
     const float small = e * big;
     return s < 0.0f ? make_float2(small, big) : make_float2(big, small);        // a NaN goes on: both are NaN
 }
+// act(a) * u.  In bf16 as a / (1 + exp(-F)): three instructions fewer than by sigmoid(); where it is below 2^-126 it is 0.
 template <class T>
-__device__ __forceinline__ float gated(float a, float u, int gate) { return a * sigmoid<T>(a, gate).x * u; }
+__device__ __forceinline__ float gated(float a, float u, int gate)
+{
+    if constexpr (sizeof(T) == 2) {
+        const float s = gate == GATE_GELU ? __builtin_fmaf(GELU_SLOPE * GELU_CUBIC * a * a, a, GELU_SLOPE * a) : a;
+        return a * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.44269504f * s)) * u;
+    } else {
+        return a * sigmoid<T>(a, gate).x * u;
+    }
+}
 
 // Tiles go to the eight XCDs in turn: each takes a run of them, eight token tiles by as many channel tiles as fit, which share their rows in its L2.
 __device__ __forceinline__ int2 tile_place(int id, int all, int tiles_t, int tiles_c)
@@ -65,9 +74,10 @@ __global__ __launch_bounds__(PRODUCT_THREADS, WC * WT > 4 ? 1 : 2) void k_gated(
     using B = RowsOperand<T, 2 * WT>;
     constexpr int PAIRS = WC / 2, TILE_C = 64 * PAIRS, TILE_T = 64 * WT;
     __shared__ __align__(16) char lds[2 * (A::BYTES + B::BYTES)];
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, wave_c = wave / 2, wave_t = wave % 2;
     const int2 place = tile_place(blockIdx.x, g.tiles_t * g.tiles_c, g.tiles_t, g.tiles_c);
     const int64_t t0 = (int64_t)place.x * TILE_T, c0 = (int64_t)place.y * TILE_C;
-    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, wave_c = wave / 2, wave_t = wave % 2;
+    const int64_t steps = (g.n + STEP<T> - 1) / STEP<T>, safe = min(A::safe(g.n, g.w_stride, g.f + TILE_C), B::safe(g.n, g.x_stride, TILE_T));
     // Block b of the weight's rows: wavefronts' blocks one after the other, in each the gate's, then the other projection's of the same channels.
     const auto w_row = [&](int b) {
         const int64_t c = min(c0 + (b / WC * PAIRS + b % WC % PAIRS) * 32 + A::row(), g.f - 1);
@@ -77,7 +87,6 @@ __global__ __launch_bounds__(PRODUCT_THREADS, WC * WT > 4 ? 1 : 2) void k_gated(
     A a;
     B b;
     f32x16 acc[WC][WT];
-    const int64_t steps = (g.n + STEP<T> - 1) / STEP<T>, safe = min(A::safe(g.n, g.w_stride, g.f + TILE_C), B::safe(g.n, g.x_stride, TILE_T));
     a.begin(g.w, g.w_stride, 0, c0, w_row);
     b.begin(g.x, g.x_stride, 0, t0, x_row);
     product_steps<T, WC, WT>(
@@ -105,16 +114,18 @@ __global__ __launch_bounds__(PRODUCT_THREADS, WC * WT > 4 ? 1 : 2) void k_gated(
             const bool there = INSIDE || lane % 32 < rows;
 #pragma unroll
             for (int i = 0; i < PAIRS; ++i) {
-                float z[2][8];
+                float z[16];
 #pragma unroll
-                for (int p = 0; p < 2; ++p) {
-                    float va[8], vu[8];
-                    const int c = 32 * i + 16 * p + lane / 32 * 8;
-                    eight_channels(acc[i][j], p, va);
-                    eight_channels(acc[i + PAIRS][j], p, vu);
+                for (int r = 0; r < 4; ++r) {
+                    float va[4], vu[4];
+                    const int c = 32 * i + run_channel(lane, r);
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) z[p][k] = gated<T>(va[k], vu[k], g.gate);
-                    if (g.z) Rows::put(mine, lane, c, z[p]);
+                    for (int k = 0; k < 4; ++k) {
+                        va[k] = acc[i][j][4 * r + k];
+                        vu[k] = acc[i + PAIRS][j][4 * r + k];
+                        z[4 * r + k] = gated<T>(va[k], vu[k], g.gate);
+                    }
+                    if (g.z) Rows::put(mine, lane, c, z + 4 * r);
                     if (g.pre) {
                         Rows::put(mine + Rows::BYTES, lane, c, va);
                         Rows::put(mine + 2 * Rows::BYTES, lane, c, vu);
@@ -124,18 +135,19 @@ __global__ __launch_bounds__(PRODUCT_THREADS, WC * WT > 4 ? 1 : 2) void k_gated(
                     // a group of 32 channels: lanes l and l + 32, sixteen values each
                     unsigned top = 0;
 #pragma unroll
-                    for (int p = 0; p < 2; ++p)
-#pragma unroll
-                        for (int k = 0; k < 8; ++k) {
-                            if (!INSIDE && 32 * i + 16 * p + lane / 32 * 8 + k >= left) z[p][k] = 0.0f;
-                            top = larger(top, __float_as_uint(z[p][k]) & 0x7fffffffu);
-                        }
+                    for (int k = 0; k < 16; ++k) {
+                        if (!INSIDE && 32 * i + run_channel(lane, k / 4) + k % 4 >= left) z[k] = 0.0f;
+                        top = larger(top, __float_as_uint(z[k]) & 0x7fffffffu);
+                    }
                     const u32x2 s = __builtin_amdgcn_permlane32_swap(top, top, false, false);
                     const unsigned byte = scale_byte(__uint_as_float(larger(s.x, s.y)));
                     if (there) {
                         const int64_t t = t1 + lane % 32;
 #pragma unroll
-                        for (int p = 0; p < 2; ++p) g.act.template put_codes<!INSIDE>(t, c1 + 32 * i + 16 * p + lane / 32 * 8, g.f, z[p], byte);
+                        for (int p = 0; p < 2; ++p) {
+                            const int64_t c = c1 + 32 * i + run_channel(lane, 2 * p);
+                            g.act.template put_two_fours<!INSIDE>(t, c, c + 8, g.f, z + 8 * p, byte);
+                        }
                         if (lane < 32) *g.act.scale_at(t, c1 + 32 * i) = (uint8_t)byte;
                     }
                 }
@@ -300,20 +312,20 @@ __global__ __launch_bounds__(PRODUCT_THREADS, WC * WT > 4 ? 1 : 2) void k_input_
     using B = RowsOperand<T, 2 * WT>;
     constexpr int TILE_C = 64 * WC, TILE_T = 64 * WT;
     __shared__ __align__(16) char lds[2 * (A::BYTES + B::BYTES)];
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, wave_c = wave / 2, wave_t = wave % 2;
     const int tiles = g.tiles_t * g.tiles_c, split = blockIdx.x / tiles;
     const int2 place = tile_place(blockIdx.x % tiles, tiles, g.tiles_t, g.tiles_c);
     const int64_t t0 = (int64_t)place.x * TILE_T, c0 = (int64_t)place.y * TILE_C;
-    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, wave_c = wave / 2, wave_t = wave % 2;
+    const int64_t steps = (g.k + STEP<T> - 1) / STEP<T>, first = steps * split / g.splits, last = steps * (split + 1) / g.splits;
+    const int64_t safe = min(last, min(A::safe(g.k, g.w_stride, c0, g.n), B::safe(g.k, g.dpre_stride, TILE_T)));
     const auto row = [&](int b) { return min(t0 + 32 * b + B::row(), g.rows - 1); };
     A a;
     B b;
     f32x16 acc[WC][WT];
-    const int64_t steps = (g.k + STEP<T> - 1) / STEP<T>, safe = min(A::safe(g.k, g.w_stride, c0, g.n), B::safe(g.k, g.dpre_stride, TILE_T));
-    const int64_t first = steps * split / g.splits, last = steps * (split + 1) / g.splits;
     a.begin(g.w, g.w_stride, first * STEP<T>, c0, g.n);
     b.begin(g.dpre, g.dpre_stride, first * STEP<T>, t0, row);
     product_steps<T, WC, WT>(
-        a, b, lds, first, last, min(last, safe), wave_c, wave_t, acc,
+        a, b, lds, first, last, safe, wave_c, wave_t, acc,
         [&] {
             a.next(g.w_stride);
             b.next();
@@ -336,10 +348,11 @@ __global__ __launch_bounds__(PRODUCT_THREADS, WC * WT > 4 ? 1 : 2) void k_input_
 #pragma unroll
             for (int i = 0; i < WC; ++i)
 #pragma unroll
-                for (int p = 0; p < 2; ++p) {
-                    float v[8];
-                    eight_channels(acc[i][j], p, v);
-                    Rows::put(mine, lane, 32 * i + 16 * p + lane / 32 * 8, v);
+                for (int r = 0; r < 4; ++r) {
+                    float v[4];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) v[k] = acc[i][j][4 * r + k];
+                    Rows::put(mine, lane, 32 * i + run_channel(lane, r), v);
                 }
             Rows::template flush<INSIDE>(mine, lane, to + t1 * stride + c1, stride, rows, left);
         }

@@ -320,13 +320,6 @@ struct ActRef {
     {
         const unsigned byte = group_scale(v);
         if (LAST && i >= groups * GROUP) return;
-        put_codes<LAST>(row, i, n, v, byte);
-        if (i % GROUP == 0) *scale_at(row, i) = (uint8_t)byte;
-    }
-    // The codes alone, of values whose group has this scale byte.
-    template <bool LAST = true>
-    __device__ __forceinline__ void put_codes(int64_t row, int64_t i, int64_t n, const float *v, unsigned byte) const
-    {
         u32x2 c = codes_of(v, byte);
         if (LAST && byte == SCALE_NAN && i + 8 > n) {       // the padding stays 0
             const int left = (int)max((int64_t)0, n - i);
@@ -335,6 +328,20 @@ struct ActRef {
             c.y &= (unsigned)(keep >> 32);
         }
         *reinterpret_cast<u32x2 *>(code_at(row, i)) = c;
+        if (i % GROUP == 0) *scale_at(row, i) = (uint8_t)byte;
+    }
+    // The codes of four values from element i on and four from element j on (multiples of 4).
+    template <bool LAST = true>
+    __device__ __forceinline__ void put_two_fours(int64_t row, int64_t i, int64_t j, int64_t n, const float *v, unsigned byte) const
+    {
+        u32x2 c = codes_of(v, byte);
+        if (LAST && byte == SCALE_NAN) {
+            const auto keep = [&](int64_t at) { return at + 4 <= n ? ~0u : at >= n ? 0u : ~0u >> (32 - 8 * (int)(n - at)); };
+            c.x &= keep(i);
+            c.y &= keep(j);
+        }
+        *reinterpret_cast<unsigned *>(code_at(row, i)) = c.x;
+        *reinterpret_cast<unsigned *>(code_at(row, j)) = c.y;
     }
     template <bool LAST = true>
     __device__ __forceinline__ void get(int64_t row, int64_t i, float *v) const

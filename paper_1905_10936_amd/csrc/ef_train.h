@@ -46,25 +46,54 @@ void launch_gated(const ef::GatedArgs &a, hipStream_t s)
     }
 }
 
+// How the product of the backward pass is cut: the tile (64 wc channels by 64 wt tokens) and the parts along what is summed over.
+struct InputCut {
+    int wc, wt, splits;
+};
+
+// The least of a sum of what was measured (bf16, us): a step of a tile with all CUs at it, a workgroup's beginning and end, and for parts a launch more and their bytes at
+// 4.5 TB/s.  fp32 steps take five times as long.
+InputCut input_cut(int type, int64_t rows, int64_t n, int64_t steps)
+{
+    struct Shape { int wc, wt, on_cu; double step, base; };
+    static constexpr Shape SHAPES[3] = {{4, 4, 1, 1.5, 10.0}, {4, 2, 1, 0.85, 7.0}, {2, 2, 2, 1.1, 6.0}};
+    InputCut best{};
+    double least = 0.0;
+    for (const Shape &c : SHAPES) {
+        const int64_t tiles = ceil_div(rows, 64 * c.wt) * ceil_div(n, 64 * c.wc), slots = 256 * c.on_cu;
+        for (int64_t splits = 1; splits <= 64 && splits <= steps; ++splits) {
+            if (splits > 1 && splits * rows * n > PART_FLOATS) break;
+            const double rounds = (double)ceil_div(tiles * splits, slots);
+            const double cost = rounds * ((double)ceil_div(steps, splits) * c.step * (type == EF_TYPE_BF16 ? 1.0 : 5.0) + c.base) +
+                                (splits > 1 ? 4.0 + (double)(splits + 1) * (double)(rows * n) * 4.0 / 4.5e6 : 0.0);
+            if (!best.splits || cost < least) {
+                best = InputCut{c.wc, c.wt, (int)splits};
+                least = cost;
+            }
+        }
+    }
+    return best;
+}
+
 template <class T, int WC, int WT>
 void launch_input_grad(ef::InputGradArgs a, hipStream_t s)
 {
     a.tiles_t = (int)ceil_div(a.rows, 64 * WT);
     a.tiles_c = (int)ceil_div(a.n, 64 * WC);
-    const int64_t tiles = (int64_t)a.tiles_t * a.tiles_c, steps = ceil_div(a.k, ef::STEP<T>);
-    int64_t splits = std::max<int64_t>(1, std::min((WC * WT > 4 ? 256 : 512) / tiles, steps / 4));
-    splits = std::min(splits, PART_FLOATS / std::max<int64_t>(1, a.rows * a.n));
-    a.splits = (int)std::max<int64_t>(1, splits);
-    hipLaunchKernelGGL((ef::k_input_grad<T, WC, WT>), dim3((unsigned)(tiles * a.splits)), dim3(ef::PRODUCT_THREADS), 0, s, a);
+    hipLaunchKernelGGL((ef::k_input_grad<T, WC, WT>), dim3((unsigned)(a.tiles_t * a.tiles_c * a.splits)), dim3(ef::PRODUCT_THREADS), 0, s, a);
     if (a.splits > 1)
         hipLaunchKernelGGL(ef::k_join_input_grad<T>, dim3((unsigned)ceil_div(a.rows * ceil_div(a.n, 8), 256)), dim3(256), 0, s, a);
 }
 
 template <class T>
-void launch_input_grad(const ef::InputGradArgs &a, hipStream_t s)
+void launch_input_grad(ef::InputGradArgs a, hipStream_t s)
 {
-    if (ceil_div(a.rows, 256) * ceil_div(a.n, 256) >= 192)
+    const InputCut c = input_cut(sizeof(T) == 2 ? EF_TYPE_BF16 : EF_TYPE_FP32, a.rows, a.n, ceil_div(a.k, ef::STEP<T>));
+    a.splits = c.splits;
+    if (c.wc == 4 && c.wt == 4)
         launch_input_grad<T, 4, 4>(a, s);
+    else if (c.wc == 4)
+        launch_input_grad<T, 4, 2>(a, s);
     else
         launch_input_grad<T, 2, 2>(a, s);
 }
