@@ -255,7 +255,7 @@ struct GradSchedule {
     int piece[REGIONS * PRODUCTS + 1] = {}, reads[PRODUCTS + 1] = {};
     constexpr GradSchedule()
     {
-        constexpr int SLOTS = (REGIONS - 1) * PRODUCTS, EARLY = PRODUCTS * 3 / 4;
+        constexpr int SLOTS = (REGIONS - 1) * PRODUCTS, EARLY = PRODUCTS > 1 ? PRODUCTS * 3 / 4 : 1;
         for (int k = 0; k <= REGIONS * PRODUCTS; ++k) piece[k] = k < SLOTS ? k * PIECES / SLOTS : PIECES;
         for (int m = 0; m <= PRODUCTS; ++m) reads[m] = m < EARLY ? (m * HALVES + EARLY - 1) / EARLY : HALVES;
     }

@@ -2,6 +2,7 @@
 // ef_layers.h, whose helpers it uses.
 #pragma once
 #include <new>
+#include <utility>
 #include <vector>
 
 #include "ef_clip.h"
@@ -12,6 +13,21 @@
 namespace {
 
 constexpr int64_t TILES_MAX = 0x1ffffff;
+
+// A tile of a product, 64 wc channels by 64 wt tokens, and what it was measured to take: a step (128 bytes of what is summed over) `alone` us with few workgroups
+// on the GPU and `loaded` us with as many as it holds (`most` on a CU; more slow the others down with the square of their share), a workgroup's beginning
+// and end `over`.
+struct TileShape {
+    int wc, wt, most;
+    double alone, loaded, over;
+    // `groups` workgroups of `steps` each
+    double cost(int64_t groups, int64_t steps) const
+    {
+        const int64_t round = 256 * most, full = groups / round, rest = groups % round;
+        const double share = (double)rest / (double)round;
+        return 3.0 + (double)full * ((double)steps * loaded + over) + (rest ? (double)steps * (alone + (loaded - alone) * share * share) + over : 0.0);
+    }
+};
 
 template <class T, int WC, int WT>
 void launch_gated(ef::GatedArgs a, hipStream_t s)
@@ -29,42 +45,54 @@ void launch_gated_few(ef::GatedArgs a, hipStream_t s)
     hipLaunchKernelGGL((ef::k_gated_few<T, CHANNELS>), dim3((unsigned)(a.tiles_t * a.tiles_c)), dim3(64 * ef::FEW_WAVES), 0, s, a);
 }
 
-constexpr int64_t FEW_ROWS = 64;
-
+// The least of the costs, the same whatever outputs are asked for: each then has the same bits.  1024 -> 4096 channels in bf16, us for 32, 128, 512, 1024 and 2048 tokens: few tokens 7.5, 24, 80; tiles of 64 tokens 9.0, 9.1, 14.4, 25.5, 47;
+// of 128 10.7, 11.2, 13.2, 21.1, 38; of 256 23, 28, 27, 29.5, 36.  In fp32 15, 46, 158; 38, 39, 74, 147, 274; 66, 67, 73, 139, 258; 235 to 253.
 template <class T>
 void launch_gated(const ef::GatedArgs &a, hipStream_t s)
 {
-    if (a.rows <= FEW_ROWS) {
-        if (a.act.codes)
-            launch_gated_few<T, 32>(a, s);
-        else
-            launch_gated_few<T, 16>(a, s);
-    } else if (ceil_div(a.rows, 256) * ceil_div(a.f, 128) >= 192) {
-        launch_gated<T, 4, 4>(a, s);
-    } else {
-        launch_gated<T, 2, 2>(a, s);
+    static constexpr TileShape SHAPES[2][3] = {{{4, 4, 1, 7.1, 7.5, 7.0}, {2, 2, 2, 1.9, 4.2, 1.5}, {2, 1, 2, 1.05, 2.15, 1.0}},
+                                               {{4, 4, 1, 0.9, 1.5, 7.0}, {2, 2, 2, 0.38, 1.1, 1.5}, {2, 1, 2, 0.3, 0.63, 1.0}}};
+    const int64_t steps = ceil_div(a.n, ef::STEP<T>);
+    const double round = sizeof(T) == 2 ? 1.6 + 3.9 * (double)a.n / 1024.0 : 1.5 + 9.5 * (double)a.n / 1024.0;
+    double least = 1.5 + round * (double)ceil_div(ceil_div(a.rows, 32) * ceil_div(a.f, 16), 256);
+    int best = -1;
+    for (int i = 0; i < 3; ++i) {
+        const TileShape &c = SHAPES[sizeof(T) == 2][i];
+        const double cost = c.cost(ceil_div(a.rows, 64 * c.wt) * ceil_div(a.f, 32 * c.wc), steps);
+        if (cost < least) {
+            least = cost;
+            best = i;
+        }
     }
+    if (best == 0)
+        launch_gated<T, 4, 4>(a, s);
+    else if (best == 1)
+        launch_gated<T, 2, 2>(a, s);
+    else if (best == 2)
+        launch_gated<T, 2, 1>(a, s);
+    else if (a.act.codes)
+        launch_gated_few<T, 32>(a, s);
+    else
+        launch_gated_few<T, 16>(a, s);
 }
 
-// How the product of the backward pass is cut: the tile (64 wc channels by 64 wt tokens) and the parts along what is summed over.
+// How the product of the backward pass is cut: the tile and the parts along what is summed over; parts cost a launch more and their bytes at 4.5 TB/s.  us, each
+// tile with its best number of parts, 256 x 256, 256 x 128, 128 x 128 and 64 x 64: bf16, 8192 summed over, 4096 x 1024 86, 76, 77, 102; 300 x 2048 33, 28, 27, 25; 64 x 1024 26,
+// 20, 16, 13; fp32, 2062 summed over, 777 x 515 77, 54, 46, 32.
 struct InputCut {
     int wc, wt, splits;
 };
-
-// The least of a sum of what was measured (bf16, us): a step of a tile with all CUs at it, a workgroup's beginning and end, and for parts a launch more and their bytes at
-// 4.5 TB/s.  fp32 steps take five times as long.
 InputCut input_cut(int type, int64_t rows, int64_t n, int64_t steps)
 {
-    struct Shape { int wc, wt, on_cu; double step, base; };
-    static constexpr Shape SHAPES[3] = {{4, 4, 1, 1.5, 10.0}, {4, 2, 1, 0.85, 7.0}, {2, 2, 2, 1.1, 6.0}};
+    static constexpr TileShape SHAPES[2][4] = {{{4, 4, 1, 7.1, 7.3, 7.0}, {4, 2, 1, 3.7, 3.8, 5.0}, {2, 2, 2, 2.0, 3.8, 2.0}, {1, 1, 4, 0.57, 1.9, 1.0}},
+                                               {{4, 4, 1, 1.1, 1.5, 7.0}, {4, 2, 1, 0.65, 0.95, 5.0}, {2, 2, 2, 0.43, 1.1, 2.0}, {1, 1, 4, 0.28, 0.84, 1.0}}};
     InputCut best{};
     double least = 0.0;
-    for (const Shape &c : SHAPES) {
-        const int64_t tiles = ceil_div(rows, 64 * c.wt) * ceil_div(n, 64 * c.wc), slots = 256 * c.on_cu;
+    for (const TileShape &c : SHAPES[type == EF_TYPE_BF16]) {
+        const int64_t tiles = ceil_div(rows, 64 * c.wt) * ceil_div(n, 64 * c.wc);
         for (int64_t splits = 1; splits <= 64 && splits <= steps; ++splits) {
             if (splits > 1 && splits * rows * n > PART_FLOATS) break;
-            const double rounds = (double)ceil_div(tiles * splits, slots);
-            const double cost = rounds * ((double)ceil_div(steps, splits) * c.step * (type == EF_TYPE_BF16 ? 1.0 : 5.0) + c.base) +
+            const double cost = c.cost(tiles * splits, ceil_div(steps, splits)) +
                                 (splits > 1 ? 4.0 + (double)(splits + 1) * (double)(rows * n) * 4.0 / 4.5e6 : 0.0);
             if (!best.splits || cost < least) {
                 best = InputCut{c.wc, c.wt, (int)splits};
@@ -90,12 +118,14 @@ void launch_input_grad(ef::InputGradArgs a, hipStream_t s)
 {
     const InputCut c = input_cut(sizeof(T) == 2 ? EF_TYPE_BF16 : EF_TYPE_FP32, a.rows, a.n, ceil_div(a.k, ef::STEP<T>));
     a.splits = c.splits;
-    if (c.wc == 4 && c.wt == 4)
+    if (c.wt == 4)
         launch_input_grad<T, 4, 4>(a, s);
     else if (c.wc == 4)
         launch_input_grad<T, 4, 2>(a, s);
-    else
+    else if (c.wc == 2)
         launch_input_grad<T, 2, 2>(a, s);
+    else
+        launch_input_grad<T, 1, 1>(a, s);
 }
 
 template <class T, int LANES, int HELD>
@@ -237,25 +267,34 @@ try {
             if (!aligned(p, type_size(types[i]))) return EF_ERR_ALIGN;
         }
     }
+    if (n_workers > 0xffff) return EF_ERR_SIZE;
     if (flat && n_workers > 1 && (flat_stride < total || flat_stride > INT64_MAX / 8 / n_workers)) return EF_ERR_ARG;
     if (!aligned(flat, 4) || !aligned(norm, 4)) return EF_ERR_ALIGN;
-    // What is written shares nothing with what else is read or written: a list of spans by address, each marked as written or read.
-    struct Span { uintptr_t begin, end; bool written; };
-    std::vector<Span> spans;
-    spans.reserve((size_t)n_workers * ((size_t)n_tensors + 1) + 1);
-    const auto span = [&](const void *p, size_t bytes, bool written) {
-        if (p && bytes) spans.push_back({reinterpret_cast<uintptr_t>(p), reinterpret_cast<uintptr_t>(p) + bytes, written});
-    };
-    for (int w = 0; w < n_workers; ++w) {
-        for (int64_t i = 0; i < n_tensors; ++i) span(grads[(int64_t)w * n_tensors + i], (size_t)sizes[i] * type_size(types[i]), !flat);
-        if (flat) span(flat + (int64_t)w * (n_workers > 1 ? flat_stride : 0), (size_t)total * 4, true);
+    // What is written shares nothing with what else is read or written.
+    const size_t norm_bytes = (size_t)n_workers * 4, row_bytes = (size_t)total * 4;
+    const int64_t stride = n_workers > 1 ? flat_stride : 0;
+    const size_t flat_bytes = (size_t)(n_workers - 1) * (size_t)stride * 4 + row_bytes;
+    const auto bytes_of = [&](int64_t i) { return (size_t)sizes[i] * type_size(types[i]); };
+    for (int64_t i = 0; i < n_tensors * n_workers; ++i) {
+        const void *p = grads[i];
+        const size_t bytes = bytes_of(i % n_tensors);
+        if (!bytes) continue;
+        if (overlap(p, bytes, norm, norm_bytes)) return EF_ERR_ARG;
+        if (flat && overlap(p, bytes, flat, flat_bytes))
+            for (int w = 0; w < n_workers; ++w)
+                if (row_bytes && overlap(p, bytes, flat + w * stride, row_bytes)) return EF_ERR_ARG;
     }
-    span(norm, (size_t)n_workers * 4, true);
-    std::sort(spans.begin(), spans.end(), [](const Span &a, const Span &b) { return a.begin < b.begin; });
-    uintptr_t read_end = 0, written_end = 0;
-    for (const Span &s : spans) {
-        if (s.begin < written_end || (s.written && s.begin < read_end)) return EF_ERR_ARG;
-        (s.written ? written_end : read_end) = std::max(s.written ? written_end : read_end, s.end);
+    for (int w = 0; flat && w < n_workers; ++w)
+        if (row_bytes && overlap(norm, norm_bytes, flat + w * stride, row_bytes)) return EF_ERR_ARG;
+    if (!flat) {
+        // in place: no two tensors share anything
+        std::vector<std::pair<uintptr_t, uintptr_t>> spans;
+        spans.reserve((size_t)(n_tensors * n_workers));
+        for (int64_t i = 0; i < n_tensors * n_workers; ++i)
+            if (sizes[i % n_tensors]) spans.emplace_back(reinterpret_cast<uintptr_t>(grads[i]), reinterpret_cast<uintptr_t>(grads[i]) + bytes_of(i % n_tensors));
+        std::sort(spans.begin(), spans.end());
+        for (size_t i = 1; i < spans.size(); ++i)
+            if (spans[i].first < spans[i - 1].second) return EF_ERR_ARG;
     }
     const int rc = on_workspace_device(workspace);
     if (rc) return rc;
@@ -278,7 +317,7 @@ try {
     // Chunks of 2048 to 16384 places; workgroups for 4096 in all, or 2048 for a worker.
     a.chunk = std::min<int64_t>(ef::CLIP_MOST, ceil_div(count, (int64_t)ef::CLIP_GROUPS * ef::CLIP_LEAST) * ef::CLIP_LEAST);
     const int64_t groups = std::min<int64_t>(ceil_div(count, a.chunk), std::max<int64_t>(256, std::min<int64_t>(ef::CLIP_GROUPS, 2 * ef::CLIP_GROUPS / n_workers)));
-    if (words + groups * n_workers > PART_FLOATS / 2 || words > 0x7fffffff || n_workers > 0xffff) return EF_ERR_SIZE;
+    if (words + groups * n_workers > PART_FLOATS / 2 || words > 0x7fffffff) return EF_ERR_SIZE;
     a.tensors = (int)n;
     a.sums = reinterpret_cast<double *>(workspace->parts);
     a.flat = flat;
