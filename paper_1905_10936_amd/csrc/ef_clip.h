@@ -47,7 +47,12 @@ __global__ __launch_bounds__(CLIP_WORDS) void k_clip_words(ClipWords a)
 // Memory that no kernel writes while this one runs: read by scalar loads.
 #define EF_CONSTANT __attribute__((address_space(4)))
 
-// f(address, fp32?, first element, elements, place of the first) for each tensor's part of the workgroup's chunks.
+// Who goes through a part: the workgroup, or a wavefront.
+struct ClipTeam {
+    int me, all;
+};
+
+// f(address, fp32?, first element, elements, place of the first, who) for each tensor's part of the workgroup's chunks.
 template <bool BACKWARDS, class F>
 __device__ __forceinline__ void each_part(const ClipArgs &a, const EF_CONSTANT uint64_t *words, F f)
 {
@@ -63,10 +68,16 @@ __device__ __forceinline__ void each_part(const ClipArgs &a, const EF_CONSTANT u
                 hi = mid;
         }
         lo = __builtin_amdgcn_readfirstlane(lo);
-        for (int64_t at = begin; at < end; ++lo) {
+        for (int64_t at = begin, part = 0; at < end; ++lo, ++part) {
             const int64_t first = (int64_t)words[lo], next = min(end, lo + 1 < a.tensors ? (int64_t)words[lo + 1] : a.length);
             const uint64_t p = words[(1 + (int)blockIdx.y) * a.tensors + lo];
-            f(reinterpret_cast<void *>(p & ~1ull), (p & 1) != 0, at - first, (int)(next - at), at);
+            // short parts one behind the other wait for memory each time: every fourth is a wavefront's (two workers of 65 tensors, 272 k
+            // elements: 15.2 us, 13.1 this way)
+            const int n = (int)(next - at), wave = (int)__builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+            if (n > 512)
+                f(reinterpret_cast<void *>(p & ~1ull), (p & 1) != 0, at - first, n, at, ClipTeam{(int)threadIdx.x, CLIP_THREADS});
+            else if ((int)(part & 3) == wave)
+                f(reinterpret_cast<void *>(p & ~1ull), (p & 1) != 0, at - first, n, at, ClipTeam{(int)threadIdx.x % 64, 64});
             at = next;
         }
     }
@@ -96,12 +107,13 @@ __device__ __forceinline__ float element(const T *p, unsigned i)
 // A part of n elements (of one chunk) in whole eights from the first 16-byte boundary of `p` on, AHEAD of them under way at a time, and what is left at its ends:
 // load(place) and use(place, what it gave) for the eights, one(place) for an element.
 template <class E, class P, class Load, class Use, class One>
-__device__ __forceinline__ void eights_of_part(const P *p, int n, Load load, Use use, One one)
+__device__ __forceinline__ void eights_of_part(const P *p, int n, ClipTeam who, Load load, Use use, One one)
 {
-    constexpr int AHEAD = 4, ROUND = 8 * CLIP_THREADS;
+    constexpr int AHEAD = 4;
+    const int ROUND = 8 * who.all;
     const int head = min(n, (int)((16 - reinterpret_cast<uintptr_t>(p) % 16) % 16 / sizeof(P)));
     const int end = head + (n - head) / 8 * 8;
-    for (int r = head + (int)threadIdx.x * 8; r < end; r += AHEAD * ROUND) {
+    for (int r = head + who.me * 8; r < end; r += AHEAD * ROUND) {
         E e[AHEAD];
         // without a branch, beyond the end the last eight again: loads behind branches are waited for one by one
 #pragma unroll
@@ -110,16 +122,16 @@ __device__ __forceinline__ void eights_of_part(const P *p, int n, Load load, Use
         for (int k = 0; k < AHEAD; ++k)
             if (r + k * ROUND < end) use((unsigned)(r + k * ROUND), e[k]);
     }
-    if ((int)threadIdx.x < head) one(threadIdx.x);
-    if ((int)threadIdx.x < n - end) one((unsigned)end + threadIdx.x);
+    if (who.me < head) one((unsigned)who.me);
+    if (who.me < n - end) one((unsigned)(end + who.me));
 }
 
 template <class T>
-__device__ __forceinline__ double squares(const T *p, int n)
+__device__ __forceinline__ double squares(const T *p, int n, ClipTeam who)
 {
     double s[2] = {0.0, 0.0};
     eights_of_part<Eight<T>>(
-        p, n,
+        p, n, who,
         [&](unsigned i) {
             Eight<T> e;
             e.load_at(p, i * (unsigned)sizeof(T));
@@ -152,8 +164,8 @@ __global__ __launch_bounds__(CLIP_THREADS) void k_clip_norm(Args args)
     const ClipArgs a = args.a;
     __shared__ double at[CLIP_THREADS / 64];
     double s = 0.0;
-    each_part<false>(a, words_of(args), [&](void *p, bool wide, int64_t i, int n, int64_t) {
-        s += wide ? squares(static_cast<const float *>(p) + i, n) : squares(static_cast<const bf16_t *>(p) + i, n);
+    each_part<false>(a, words_of(args), [&](void *p, bool wide, int64_t i, int n, int64_t, ClipTeam who) {
+        s += wide ? squares(static_cast<const float *>(p) + i, n, who) : squares(static_cast<const bf16_t *>(p) + i, n, who);
     });
     s = clip_sum(s, at);
     if (threadIdx.x == 0) a.sums[(int64_t)blockIdx.y * gridDim.x + blockIdx.x] = s;
@@ -161,10 +173,10 @@ __global__ __launch_bounds__(CLIP_THREADS) void k_clip_norm(Args args)
 
 // The product in 64 bits: next to a huge norm the factor is beyond fp32 though the products are not.
 template <class T, class To>
-__device__ __forceinline__ void scaled(const T *p, To *to, int n, double factor)
+__device__ __forceinline__ void scaled(const T *p, To *to, int n, ClipTeam who, double factor)
 {
     eights_of_part<Eight<T>>(
-        to, n,
+        to, n, who,
         [&](unsigned i) {
             Eight<T> e;
             e.load_at(p, i * (unsigned)sizeof(T));
@@ -202,17 +214,17 @@ __global__ __launch_bounds__(CLIP_THREADS) void k_clip_scale(Args args)
     const double factor = norm > (double)a.max_norm && norm < INFINITY ? (double)a.max_norm / norm : 1.0;
     if (!a.flat && factor == 1.0) return;
     // backwards: it begins where the first pass ended, with what the caches still hold
-    each_part<true>(a, words_of(args), [&](void *p, bool wide, int64_t i, int n, int64_t place) {
+    each_part<true>(a, words_of(args), [&](void *p, bool wide, int64_t i, int n, int64_t place, ClipTeam who) {
         if (a.flat) {
             float *const to = a.flat + (int64_t)worker * a.flat_stride + place;
             if (wide)
-                scaled(static_cast<const float *>(p) + i, to, n, factor);
+                scaled(static_cast<const float *>(p) + i, to, n, who, factor);
             else
-                scaled(static_cast<const bf16_t *>(p) + i, to, n, factor);
+                scaled(static_cast<const bf16_t *>(p) + i, to, n, who, factor);
         } else if (wide) {
-            scaled(static_cast<const float *>(p) + i, static_cast<float *>(p) + i, n, factor);
+            scaled(static_cast<const float *>(p) + i, static_cast<float *>(p) + i, n, who, factor);
         } else {
-            scaled(static_cast<const bf16_t *>(p) + i, static_cast<bf16_t *>(p) + i, n, factor);
+            scaled(static_cast<const bf16_t *>(p) + i, static_cast<bf16_t *>(p) + i, n, who, factor);
         }
     });
 }
