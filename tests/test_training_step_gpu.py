@@ -1,0 +1,223 @@
+"""A worker's step on all the operators together: tokens drawn, norm, gated block, head, policy loss, its backward pass, clipping and the step itself."""
+import math
+import os
+import sys
+
+import pytest
+import torch
+
+import paper_1905_10936_amd as ef
+
+sys.path.insert(0, os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples"))
+
+pytestmark = pytest.mark.gpu
+
+
+def test_gradients_with_a_gated_block():
+    """Against torch's own in fp32.  E4M3 rounds each value of a checkpoint by up to 2^-4, a fortieth in the mean square, independently: so much of a
+    gradient's norm for each checkpoint on its way (two at most), and the bf16 steps 2^-8 each."""
+    import policy_training as example
+    rows, vocab, width, inner = 500, 131, 96, 80
+    policy = example.Policy(vocab=vocab, width=width, rows=rows, seed=3, inner=inner)
+    gen = torch.Generator("cuda").manual_seed(4)
+    tokens, uniform = torch.randint(0, vocab, (rows,), device="cuda", generator=gen), torch.rand(rows, device="cuda", generator=gen)
+    actions, old = torch.empty_like(tokens), torch.empty(rows, device="cuda")
+    ef.ef_sample_tokens(policy.workspace, policy.logits(tokens), uniform, None, None, None, None, actions, old)
+    ref = old - 0.2
+    old += 0.1 * torch.randn(rows, device="cuda", generator=gen)
+    advantage = torch.randn(rows, device="cuda", generator=gen)
+    weight = torch.full((rows,), 1 / 400.0, device="cuda")
+    weight[::5] = 0.0
+    grad = torch.full((policy.d,), float("nan"), device="cuda")
+    policy.step(tokens, actions, old, ref, advantage, weight, grad)
+
+    flat = policy.params.clone().requires_grad_(True)
+    p = policy.views(flat)
+
+    def norm(v, w):
+        return v * torch.rsqrt((v * v).mean(1, keepdim=True) + example.EPS) * w
+
+    x = p["embedding"][tokens]
+    both = norm(x, p["block_norm"]) @ p["gate_up"].t()
+    a, u = both[:, :inner], both[:, inner:]
+    y = norm(x + (a * torch.sigmoid(a) * u) @ p["down"].t(), p["norm"])
+    logp = torch.log_softmax(y @ p["head"].t(), 1).gather(1, actions[:, None])[:, 0]
+    ratio, d = torch.exp(logp - old), ref - logp
+    want = -torch.minimum(ratio * advantage, ratio.clamp(1 - example.CLIP, 1 + example.CLIP) * advantage) + example.KL * (torch.expm1(d) - d)
+    (weight * want).sum().backward()
+    for name, got in policy.views(grad).items():
+        exact = policy.views(flat.grad)[name]
+        assert float((got - exact).norm()) <= 0.08 * float(exact.norm()), name
+
+    # the worker's row clipped in place is what the clipped copy holds, and as long as it is to be
+    whole, norms = grad.double().norm(), torch.empty(1, device="cuda")
+    limit = float(whole) / 3
+    copy = torch.empty(policy.d, device="cuda")
+    ef.ef_grad_clip(policy.workspace, list(policy.views(grad).values()), limit, copy, norms)
+    assert abs(float(norms) - float(whole)) <= 2.0 ** -23 * float(whole)
+    ef.ef_grad_clip(policy.workspace, [grad], limit, None, norms)
+    assert torch.equal(copy, grad) and abs(float(grad.double().norm()) - limit) <= 2.0 ** -22 * limit
+
+
+def test_it_runs_with_a_block_and_clipping():
+    import policy_training as example
+    rewards = example.train(steps=3, workers=2, say=None, inner=64, clip_norm=0.5)
+    assert len(rewards) == 3 and all(0.0 <= r <= 1.0 for r in rewards)
+
+
+def test_captured_as_one_graph():
+    """Drawing, forward and backward pass and clipping in one graph, replayed beside eager steps with other tokens in the same buffers."""
+    rows, vocab, width, inner = 192, 300, 64, 96
+    gen = torch.Generator("cuda").manual_seed(1)
+    bf = torch.bfloat16
+    ws = ef.ef_workspace_create(rows)
+    x, w, head = (torch.randn(*s, device="cuda", generator=gen).to(bf) for s in ((rows, width), (2 * inner, width), (vocab, inner)))
+    w_norm, uniform = torch.ones(width, device="cuda"), torch.rand(rows, device="cuda", generator=gen)
+    y, act, rstd = torch.empty_like(x), torch.zeros(ef.ef_act_bytes(rows, width), dtype=torch.uint8, device="cuda"), torch.empty(rows, device="cuda")
+    pre, z, dpre, dx = (torch.zeros(rows, k, device="cuda", dtype=bf) for k in (2 * inner, inner, 2 * inner, width))
+    logits, dz = torch.zeros(rows, vocab, device="cuda", dtype=bf), torch.zeros(rows, inner, device="cuda", dtype=bf)
+    tokens, logp, advantage = torch.zeros(rows, dtype=torch.int64, device="cuda"), torch.zeros(rows, device="cuda"), torch.randn(rows, device="cuda", generator=gen)
+    loss, dw, flat, norm = torch.zeros(1, device="cuda"), torch.zeros(2 * inner, width, device="cuda"), torch.zeros(2 * inner * width + width * rows, device="cuda"), torch.zeros(1, device="cuda")
+
+    def step():
+        ef.ef_norm_forward(x, None, w_norm, 1e-6, None, y, act, rstd)
+        ef.ef_gated_forward(y, w, ef.EF_GATE_GELU, pre, z, None)
+        torch.mm(z, head.t(), out=logits)
+        ef.ef_sample_tokens(ws, logits, uniform, None, None, None, None, tokens, logp)
+        ef.ef_policy_loss(ws, logits, tokens, None, None, advantage, None, 0.2, 0.2, 0.0, None, None, loss, logits)
+        torch.mm(logits, head, out=dz)
+        ef.ef_gated_backward(ws, dz, pre, w, ef.EF_GATE_GELU, dpre, dx)
+        ef.ef_weight_grad(ws, dpre, act, w_norm, dw)
+        ef.ef_grad_clip(ws, [dw, dx], 1.0, flat, norm)
+
+    outputs = (tokens, logp, loss, dpre, dx, dw, flat, norm)
+    stream, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    with torch.cuda.stream(stream):
+        step()
+        torch.cuda.synchronize()
+        with torch.cuda.graph(graph, stream=stream):
+            step()
+    for _ in range(3):
+        x.copy_(torch.randn(rows, width, device="cuda", generator=gen))
+        uniform.uniform_(generator=gen)
+        step()
+        want = [t.clone() for t in outputs]
+        for t in outputs:
+            t.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        for t, v in zip(outputs, want):
+            assert torch.equal(t, v)
+        assert math.isfinite(float(norm)) and float(norm) > 1.0
+
+
+def test_the_native_calls_are_taken_and_give_the_same_bits(monkeypatch):
+    """csrc/ef_binding.cpp against the path through ctypes, for every form of the arguments."""
+    ef.lib()
+    answers = []
+
+    class Recorder:
+        def __init__(self, native):
+            self.native = native
+
+        def __getattr__(self, name):
+            def call(*args):
+                rc = getattr(self.native, name)(*args)
+                answers.append((name, rc is not None))
+                return rc
+            return call
+
+    def run(bare, dtype, rows, pad):
+        gen = torch.Generator("cuda").manual_seed(3)
+        n, f = 40, 50
+
+        def matrix(width):
+            return torch.randn(rows, width + pad, device="cuda", generator=gen).to(dtype)[:, :width]
+
+        ws, x, w = ef.ef_workspace_create(rows), matrix(n), torch.randn(2 * f, n, device="cuda", generator=gen).to(dtype)
+        pre, z, dpre, dx, act = matrix(2 * f), matrix(f), matrix(2 * f), matrix(n), torch.zeros(ef.ef_act_bytes(rows, f), dtype=torch.uint8, device="cuda")
+        ef.ef_gated_forward(x, w, ef.EF_GATE_SILU, pre, z, None if bare else act)
+        ef.ef_gated_backward(ws, z, pre, w, ef.EF_GATE_SILU, dpre, None if bare else dx)
+        u = torch.rand(rows, device="cuda", generator=gen)
+        tokens, logp = torch.zeros(rows, dtype=torch.int64, device="cuda"), torch.zeros(rows, device="cuda")
+        k = torch.full((rows,), 7, dtype=torch.int32, device="cuda")
+        ef.ef_sample_tokens(ws, pre, u, None if bare else u + 0.5, None if bare else k, None if bare else u, None if bare else u * 0.1, tokens, None if bare else logp)
+        grads = [w.contiguous(), torch.randn(30, device="cuda", generator=gen)]
+        flat, norm = torch.zeros(1, 2 * f * n + 34, device="cuda"), torch.zeros(1, device="cuda")
+        ef.ef_grad_clip(ws, grads if bare else [grads], 1.0, flat, norm)
+        ef.ef_grad_clip(ws, tuple(grads), 1.0, None, norm)
+        return [t.clone() for t in (pre, z, dpre, dx, act, tokens, logp, flat, norm, *grads)]
+
+    for bare in (False, True):
+        for dtype, rows, pad in ((torch.bfloat16, 33, 0), (torch.float32, 5, 3), (torch.float32, 1, 0)):
+            answers.clear()
+            with monkeypatch.context() as m:
+                m.setattr(ef, "_native", Recorder(ef._native))
+                native = run(bare, dtype, rows, pad)
+            assert len(answers) == 5 and all(taken for _, taken in answers), answers
+            with monkeypatch.context() as m:
+                m.setattr(ef, "_native", ef._ThroughCtypes())
+                for a, b in zip(native, run(bare, dtype, rows, pad)):
+                    assert torch.equal(a, b)
+
+
+def test_refusals_through_either():
+    ws = ef.ef_workspace_create(4)
+    x, w, z, v = torch.zeros(4, 8, device="cuda"), torch.zeros(6, 8, device="cuda"), torch.zeros(4, 3, device="cuda"), torch.zeros(4, device="cuda")
+    pre, tokens = torch.zeros(4, 6, device="cuda"), torch.zeros(4, dtype=torch.int64, device="cuda")
+    for call, error in (
+            (lambda: ef.ef_gated_forward(x, w.bfloat16(), 0, None, z, None), TypeError), (lambda: ef.ef_gated_forward(x, w[:, :7], 0, None, z, None), TypeError),
+            (lambda: ef.ef_gated_forward(x, w, 0, z, z, None), TypeError), (lambda: ef.ef_gated_forward(x, w, 2, None, z, None), ef.EfError),
+            (lambda: ef.ef_gated_forward(x, w, 0, None, None, None), ef.EfError), (lambda: ef.ef_gated_forward(x, w, 0, None, x[:, :3], None), ef.EfError),
+            (lambda: ef.ef_gated_forward(x.t(), w, 0, None, z, None), TypeError),
+            (lambda: ef.ef_gated_backward(ws, z, pre, w, 0, None, x), ef.EfError), (lambda: ef.ef_gated_backward(None, z, pre, w, 0, pre, x), TypeError),
+            (lambda: ef.ef_gated_backward(ws, z, pre[:, :5], w, 0, pre, x), TypeError),
+            (lambda: ef.ef_sample_tokens(ws, x, v.double(), None, None, None, None, tokens, None), TypeError),
+            (lambda: ef.ef_sample_tokens(ws, x, v, None, tokens, None, None, tokens, None), TypeError),
+            (lambda: ef.ef_sample_tokens(ws, x, v, None, None, None, None, None, v), ef.EfError),
+            (lambda: ef.ef_sample_tokens(ws, x, None, None, None, None, None, tokens, None), ef.EfError),
+            (lambda: ef.ef_sample_tokens(ws, torch.zeros(5, 8, device="cuda"), torch.zeros(5, device="cuda"), None, None, None, None, tokens.new_zeros(5), None), ef.EfError),
+            (lambda: ef.ef_grad_clip(ws, [x.half()], 1.0, None, v[:1]), TypeError), (lambda: ef.ef_grad_clip(ws, [x.t()], 1.0, None, v[:1]), TypeError),
+            (lambda: ef.ef_grad_clip(ws, [[x], [v]], 1.0, None, v[:2]), TypeError), (lambda: ef.ef_grad_clip(ws, [x], 1.0, v, v[:1]), TypeError),
+            (lambda: ef.ef_grad_clip(ws, [x, x], 1.0, None, v[:1]), ef.EfError), (lambda: ef.ef_grad_clip(ws, [x], -1.0, None, v[:1]), ef.EfError),
+            (lambda: ef.ef_grad_clip(ws, [x], 1.0, None, None), ef.EfError), (lambda: ef.ef_grad_clip(ws, [x], 1.0, None, v), TypeError),
+            (lambda: ef.ef_grad_clip(ws, [x], 1.0, x.view(-1), v[:1]), ef.EfError)):
+        with pytest.raises(error):
+            call()
+    ws.close()
+    with pytest.raises(ef.EfError) as e:
+        ef.ef_sample_tokens(ws, x, v, None, None, None, None, tokens, None)
+    assert e.value.code == ef.EF_ERR_NULL
+
+
+def test_two_workspaces_on_two_streams():
+    """Calls that share nothing, at the same time."""
+    gen = torch.Generator("cuda").manual_seed(2)
+    jobs = []
+    for _ in range(2):
+        rows, n, f = 96, 128, 2000
+        dz, pre, w = (torch.randn(*s, device="cuda", generator=gen).bfloat16() for s in ((rows, f), (rows, 2 * f), (2 * f, n)))
+        l, u, g = torch.randn(64, 50000, device="cuda", generator=gen), torch.rand(64, device="cuda", generator=gen), [torch.randn(3000000, device="cuda", generator=gen)]
+        jobs.append((ef.ef_workspace_create(rows), dz, pre, w, torch.empty_like(pre), torch.empty(rows, n, device="cuda", dtype=torch.bfloat16), l, u,
+                     torch.full((64,), 0.9, device="cuda"), torch.zeros(64, dtype=torch.int64, device="cuda"), torch.zeros(64, device="cuda"), g,
+                     torch.zeros(3000000, device="cuda"), torch.zeros(1, device="cuda")))
+
+    def run(ws, dz, pre, w, dpre, dx, l, u, p, tokens, logp, g, flat, norm):
+        ef.ef_gated_backward(ws, dz, pre, w, ef.EF_GATE_SILU, dpre, dx)
+        ef.ef_sample_tokens(ws, l, u, None, None, p, None, tokens, logp)
+        ef.ef_grad_clip(ws, g, 1.0, flat, norm)
+
+    want = []
+    for job in jobs:
+        run(*job)
+        want.append([t.clone() for t in (job[4], job[5], job[9], job[10], job[12], job[13])])
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in jobs]
+    for _ in range(5):
+        for stream, job in zip(streams, jobs):
+            with torch.cuda.stream(stream):
+                run(*job)
+    torch.cuda.synchronize()
+    for job, w in zip(jobs, want):
+        for a, b in zip((job[4], job[5], job[9], job[10], job[12], job[13]), w):
+            assert torch.equal(a, b)
