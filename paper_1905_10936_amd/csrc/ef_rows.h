@@ -311,8 +311,8 @@ __device__ __forceinline__ void decode_eight(u32x2 codes, unsigned byte, float *
 struct ActRef {
     uint8_t *codes, *scales;
     int64_t groups;             // scales a row; a row of codes takes 32 times as many bytes
-    __device__ __forceinline__ uint8_t *code_at(int64_t row, int64_t i) const { return codes + row * groups * GROUP + i; }
-    __device__ __forceinline__ uint8_t *scale_at(int64_t row, int64_t i) const { return scales + row * groups + i / GROUP; }
+    __host__ __device__ __forceinline__ uint8_t *code_at(int64_t row, int64_t i) const { return codes + row * groups * GROUP + i; }
+    __host__ __device__ __forceinline__ uint8_t *scale_at(int64_t row, int64_t i) const { return scales + row * groups + i / GROUP; }
     // Eight values of a group, from element i (a multiple of 8) of a row of n on; the four lanes of a group call it together.  Without LAST they
     // all lie in the row.
     template <bool LAST = true>

@@ -158,7 +158,7 @@ struct SampleRow {
     template <class F>
     __device__ __forceinline__ void from_memory(F f) const
     {
-        constexpr int AHEAD = 4;
+        constexpr int AHEAD = HELD || sizeof(T) == 2 ? 4 : 2;       // as many as registers hold
         for (int64_t i = begin; i < end; i += AHEAD * 512) {
             Eight<T> e[AHEAD];
 #pragma unroll
@@ -600,8 +600,6 @@ __global__ __launch_bounds__(Team<LANES>::THREADS) void k_sample(SampleArgs a)
     r.powers = powers;
     r.least = -3.402823466e38f;
     r.last = 0xffffffffu;
-    // The sum of the row's masses stays below 2^52 times their grid.
-    r.grid = __builtin_amdgcn_ldexp(1.5, 64 - __builtin_clzll((unsigned long long)a.vocab));
     // The policy's own sum, in fp32's exponentials: a term's error is its own, and the sums are in 64 bits.
     double whole = 0.0;
     if (a.logp) {
@@ -627,6 +625,22 @@ __global__ __launch_bounds__(Team<LANES>::THREADS) void k_sample(SampleArgs a)
         return;
     }
     r.factor = 1.4426950408889634074 / (double)heat;
+    // The grid of the masses: their sum has to stay below 2^52 times it.  No more than as many as entries can stay, none above 1: of n, what is rounded away is below n^2 2^-54.  Where
+    // that would show, the sum itself is the bound.
+    double most = top_k > 0 ? fmin((double)top_k, (double)a.vocab) : (double)a.vocab;
+    if (most > 131072.0) {
+        const float factor = (float)fmin(r.factor, 1e30);
+        double own = 0.0, all;
+        r.row.each([&](const Eight<T> &e, unsigned) {
+            float v[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] = __builtin_amdgcn_exp2f((e[k] - top) * factor);
+            own += (double)(((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7])));
+        });
+        Of::upto(own, s.wave_sum, all);
+        most = fmin(most, 1.01 * all);
+    }
+    r.grid = __builtin_amdgcn_ldexp(1.5, __builtin_amdgcn_frexp_exp(most));
     if (top_k > 0 && top_k < a.vocab) {
         r.leave_out(top_k, mine);
         if (top_k <= Of::LISTED / 2) {

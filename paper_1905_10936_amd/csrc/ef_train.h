@@ -12,7 +12,8 @@
 
 namespace {
 
-constexpr int64_t TILES_MAX = 0x1ffffff;
+constexpr int64_t ROWS_AT_ONCE = 1 << 22;       // tokens to a launch of a product: a grid holds less than 2^32 threads
+constexpr int64_t TILES_MAX = 1 << 22;
 
 // A tile of a product, 64 wc channels by 64 wt tokens, and what it was measured to take: a step (128 bytes of what is summed over) `alone` us with few workgroups
 // on the GPU and `loaded` us with as many as it holds (`most` on a CU; more slow the others down with the square of their share), a workgroup's beginning
@@ -54,12 +55,14 @@ void launch_gated(const ef::GatedArgs &a, hipStream_t s)
                                                {{4, 4, 1, 0.9, 1.5, 7.0}, {2, 2, 2, 0.38, 1.1, 1.5}, {2, 1, 2, 0.3, 0.63, 1.0}}};
     const int64_t steps = ceil_div(a.n, ef::STEP<T>);
     const double round = sizeof(T) == 2 ? 1.6 + 3.9 * (double)a.n / 1024.0 : 1.5 + 9.5 * (double)a.n / 1024.0;
-    double least = 1.5 + round * (double)ceil_div(ceil_div(a.rows, 32) * ceil_div(a.f, 16), 256);
+    const int64_t few = ceil_div(a.rows, 32) * ceil_div(a.f, 16);
+    double least = few <= TILES_MAX ? 1.5 + round * (double)ceil_div(few, 256) : 1e30;
     int best = -1;
     for (int i = 0; i < 3; ++i) {
         const TileShape &c = SHAPES[sizeof(T) == 2][i];
-        const double cost = c.cost(ceil_div(a.rows, 64 * c.wt) * ceil_div(a.f, 32 * c.wc), steps);
-        if (cost < least) {
+        const int64_t tiles = ceil_div(a.rows, 64 * c.wt) * ceil_div(a.f, 32 * c.wc);
+        const double cost = c.cost(tiles, steps);
+        if (cost < least && tiles <= TILES_MAX) {
             least = cost;
             best = i;
         }
@@ -90,6 +93,7 @@ InputCut input_cut(int type, int64_t rows, int64_t n, int64_t steps)
     double least = 0.0;
     for (const TileShape &c : SHAPES[type == EF_TYPE_BF16]) {
         const int64_t tiles = ceil_div(rows, 64 * c.wt) * ceil_div(n, 64 * c.wc);
+        if (tiles > TILES_MAX) continue;
         for (int64_t splits = 1; splits <= 64 && splits <= steps; ++splits) {
             if (splits > 1 && splits * rows * n > PART_FLOATS) break;
             const double cost = c.cost(tiles * splits, ceil_div(steps, splits)) +
@@ -157,7 +161,8 @@ void launch_sample(const ef::SampleArgs &a, hipStream_t s)
 int gated_sizes(int64_t rows, int64_t width, int64_t inner, int type, int gate)
 {
     if (rows < 0 || rows > ROWS_MAX || width < 1 || inner < 1 || !good_type(type) || (gate != EF_GATE_SILU && gate != EF_GATE_GELU)) return EF_ERR_ARG;
-    if (width > WIDTH_MAX || inner > WIDTH_MAX || ceil_div(rows, 64) * ceil_div(std::max(width, inner), 16) > TILES_MAX) return EF_ERR_SIZE;
+    // the largest tiles of as many tokens as go into a launch: more would be beyond any memory
+    if (width > WIDTH_MAX || inner > WIDTH_MAX || ceil_div(std::min(rows, ROWS_AT_ONCE), 256) * ceil_div(std::max(width, inner), 128) > TILES_MAX) return EF_ERR_SIZE;
     return EF_OK;
 }
 
@@ -190,8 +195,18 @@ int ef_gated_forward(int64_t rows, int64_t width, int64_t inner, int type, const
     const unsigned in_place[3] = {0u, 0u, 0u};
     if (!apart(out, 3, in, 2, in_place)) return EF_ERR_ARG;
     if (!rows) return EF_OK;
-    const ef::GatedArgs a{rows, width, inner, x, x_stride, w, w_stride, gate, pre, pre_stride, z, z_stride, act_ref(act, rows, inner), 0, 0};
-    EF_BY_TYPE(type, T, launch_gated<T>(a, static_cast<hipStream_t>(stream)));
+    const ef::ActRef whole = act_ref(act, rows, inner);
+    for (int64_t first = 0; first < rows; first += ROWS_AT_ONCE) {
+        const auto from = [&](auto *p, int64_t stride) { return p ? reinterpret_cast<decltype(p)>(reinterpret_cast<uintptr_t>(p) + (size_t)(first * stride) * size) : p; };
+        ef::ActRef part = whole;
+        if (act) {
+            part.codes = whole.code_at(first, 0);
+            part.scales = whole.scale_at(first, 0);
+        }
+        const ef::GatedArgs a{std::min(rows - first, ROWS_AT_ONCE), width, inner, from(x, x_stride), x_stride, w, w_stride, gate, from(pre, pre_stride), pre_stride,
+                              from(z, z_stride), z_stride, part, 0, 0};
+        EF_BY_TYPE(type, T, launch_gated<T>(a, static_cast<hipStream_t>(stream)));
+    }
     EF_HIP(hipGetLastError());
     return EF_OK;
 }
@@ -220,8 +235,12 @@ int ef_gated_backward(ef_workspace *workspace, int64_t rows, int64_t width, int6
     });
     EF_HIP(hipGetLastError());
     if (!dx) return EF_OK;
-    const ef::InputGradArgs a{rows, width, 2 * inner, dpre, dpre_stride, w, w_stride, dx, dx_stride, 0, 0, 1, workspace->parts};
-    EF_BY_TYPE(type, T, launch_input_grad<T>(a, s));
+    for (int64_t first = 0; first < rows; first += ROWS_AT_ONCE) {
+        const auto from = [&](void *p, int64_t stride) { return static_cast<void *>(static_cast<char *>(p) + (size_t)(first * stride) * size); };
+        const ef::InputGradArgs a{std::min(rows - first, ROWS_AT_ONCE), width, 2 * inner, from(dpre, dpre_stride), dpre_stride, w, w_stride, from(dx, dx_stride), dx_stride, 0, 0, 1,
+                                  workspace->parts};
+        EF_BY_TYPE(type, T, launch_input_grad<T>(a, s));
+    }
     EF_HIP(hipGetLastError());
     return EF_OK;
 }

@@ -102,7 +102,7 @@ def ef_grad_clip(workspace, grads, max_norm, flat, norm, stream=None):
         raise TypeError("grads must be a list of tensors, or a list of such lists")
     lists = grads if grads and isinstance(grads[0], (list, tuple)) else [grads]
     sizes, types, pointers = [], [], []
-    for worker in lists:
+    for w, worker in enumerate(lists):
         if not isinstance(worker, (list, tuple)) or len(worker) != len(lists[0]):
             raise TypeError("every worker must have the same number of tensors")
         for i, t in enumerate(worker):
@@ -110,7 +110,7 @@ def ef_grad_clip(workspace, grads, max_norm, flat, norm, stream=None):
                 raise TypeError("gradients must be float32 or bfloat16 tensors")
             _here(t)
             pointers.append(_ptr(t, t.dtype, "a gradient"))
-            if worker is lists[0]:
+            if w == 0:
                 sizes.append(t.numel())
                 types.append(_TYPES[t.dtype])
             elif sizes[i] != t.numel() or types[i] != _TYPES[t.dtype]:

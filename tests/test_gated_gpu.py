@@ -243,3 +243,25 @@ def test_large_tiles(kind):
     some = np.r_[0:5, 250:260, 19990:20000]
     within(dx[some], *oracle.input_grad(exact(dpre[some]), exact(w), kind))
     within(dpre[some], *oracle.gated_slopes(exact(dz[some]), exact(pre[some]), "gelu", kind))
+
+
+def test_more_rows_than_a_launch_takes():
+    """Rows beyond 2^22 go in a second launch, checkpoint and all."""
+    rows, n, f = (1 << 22) + 70, 3, 5
+    gen = torch.Generator("cuda").manual_seed(1)
+    x, w = normal(gen, rows, n, torch.bfloat16), normal(gen, 2 * f, n, torch.bfloat16)
+    pre, z, act = blank(rows, 2 * f, torch.bfloat16), blank(rows, f, torch.bfloat16), torch.zeros(ef.ef_act_bytes(rows, f), dtype=torch.uint8, device="cuda")
+    ef.ef_gated_forward(x, w, GATES["silu"], pre, z, act)
+    some = torch.cat([torch.arange(100), torch.arange(rows - 100, rows)]).cuda()
+    z64, pre64, z_raw, z_off, pre_off = oracle.gated_forward(exact(x[some]), exact(w), "silu", "bf16")
+    within(z[some], z64, z_off)
+    within(pre[some], pre64, pre_off)
+    got = blank(rows, f, torch.bfloat16)
+    ef.ef_act_decode(act, got)
+    top = (np.abs(z64) + z_raw).max(1, keepdims=True)
+    within(got[some], z64, z_raw + (np.abs(z64) + z_raw) * 2.0 ** -4 + 2.0 ** -10 * np.maximum(top / 224.0, 2.0 ** -116))
+    ws = ef.ef_workspace_create(rows)
+    dz, dpre, dx = normal(gen, rows, f, torch.bfloat16), blank(rows, 2 * f, torch.bfloat16), blank(rows, n, torch.bfloat16)
+    ef.ef_gated_backward(ws, dz, pre, w, GATES["silu"], dpre, dx)
+    within(dpre[some], *oracle.gated_slopes(exact(dz[some]), exact(pre[some]), "silu", "bf16"))
+    within(dx[some], *oracle.input_grad(exact(dpre[some]), exact(w), "bf16"))

@@ -140,6 +140,29 @@ def test_masked_entries_and_rows_without_a_distribution(kind):
     assert logp[[0, 5, 6, 7]].tolist() == [0.0] * 4
 
 
+@pytest.mark.parametrize("kind", TYPES)
+def test_many_improbable_entries(kind):
+    """Three million entries of e^-22 each, 0.0008 in all beside the one likely one: they are drawn where u says so."""
+    vocab = 3000000
+    logits = torch.full((4, vocab), -22.0, device="cuda", dtype=TYPES[kind])
+    logits[:, 5] = 0.0
+    uniform = torch.tensor([0.5, 1 - 2.0 ** -24, 0.9995, 1 - 2.0 ** -12], device="cuda")
+    tokens = check(logits, uniform)
+    assert tokens[0] == 5 and int(tokens[1]) > vocab - 1000 and 5 < int(tokens[2]) < vocab
+    check(logits, uniform, top_p=column(4, 0.9995, "top_p"))
+    check(logits, uniform, temperature=column(4, 0.9, "temperature"))
+
+
+def test_more_rows_than_a_launch_takes():
+    """2^22 workgroups to a launch; rows of one entry or two."""
+    rows = 4 * (1 << 22) + 9
+    logits = torch.zeros(rows, 2, device="cuda", dtype=torch.bfloat16)
+    logits[:, 1] = -math.inf
+    logits[-3:] = torch.tensor([-math.inf, 0.0], device="cuda")
+    tokens, logp = draw(logits, torch.full((rows,), 0.5, device="cuda"))
+    assert not tokens[:-3].any() and tokens[-3:].tolist() == [1, 1, 1] and not logp.any()
+
+
 def test_settings_out_of_range():
     logits = torch.randn(8, 100, device="cuda")
     uniform = torch.full((8,), 0.5, device="cuda")

@@ -146,7 +146,9 @@ def test_the_native_calls_are_taken_and_give_the_same_bits(monkeypatch):
         flat, norm = torch.zeros(1, 2 * f * n + 34, device="cuda"), torch.zeros(1, device="cuda")
         ef.ef_grad_clip(ws, grads if bare else [grads], 1.0, flat, norm)
         ef.ef_grad_clip(ws, tuple(grads), 1.0, None, norm)
-        return [t.clone() for t in (pre, z, dpre, dx, act, tokens, logp, flat, norm, *grads)]
+        two, norms = torch.zeros(2, 2 * f * n + 30, device="cuda"), torch.zeros(2, device="cuda")
+        ef.ef_grad_clip(ws, [grads, grads], 0.5, two, norms)            # the same list for two workers
+        return [t.clone() for t in (pre, z, dpre, dx, act, tokens, logp, flat, norm, two, norms, *grads)]
 
     for bare in (False, True):
         for dtype, rows, pad in ((torch.bfloat16, 33, 0), (torch.float32, 5, 3), (torch.float32, 1, 0)):
@@ -154,7 +156,7 @@ def test_the_native_calls_are_taken_and_give_the_same_bits(monkeypatch):
             with monkeypatch.context() as m:
                 m.setattr(ef, "_native", Recorder(ef._native))
                 native = run(bare, dtype, rows, pad)
-            assert len(answers) == 5 and all(taken for _, taken in answers), answers
+            assert len(answers) == 6 and all(taken for _, taken in answers), answers
             with monkeypatch.context() as m:
                 m.setattr(ef, "_native", ef._ThroughCtypes())
                 for a, b in zip(native, run(bare, dtype, rows, pad)):

@@ -64,7 +64,7 @@ def input_grad(dpre, w, kind):
 
 
 def sample(v, u, heat=1.0, k=0, p=1.0, m=0.0):
-    """(tokens that are right, logp by token): one token, or the two neighbours of a border that u is next to (within 1e-9 of the whole)."""
+    """(tokens that are right, logp by token): one token, or those within 1e-9 of the whole from u, where it is next to a border."""
     if np.isnan(v).any() or v.max() in (math.inf, -math.inf) or not 0 <= u < 1 or not 0 <= heat < math.inf or math.isnan(p) or math.isnan(m):
         return {-1}, {-1: math.nan}
     order = np.lexsort((np.arange(v.size), -v))
@@ -86,6 +86,6 @@ def sample(v, u, heat=1.0, k=0, p=1.0, m=0.0):
         stay = np.sort(first[keep])
         with np.errstate(over="ignore"):
             c = np.cumsum(np.exp((v[stay] - top) / heat))
-        for t in (u * c[-1] - 1e-9 * c[-1], u * c[-1], u * c[-1] + 1e-9 * c[-1]):
-            right.add(int(stay[min(np.searchsorted(c, t, side="right"), len(stay) - 1)]))
+        low, high = (min(int(np.searchsorted(c, (u + off) * c[-1], side="right")), len(stay) - 1) for off in (-1e-9, 1e-9))
+        right.update(stay[low:high + 1].tolist())
     return right, {t: logp(t) for t in right}
