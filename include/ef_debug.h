@@ -106,6 +106,15 @@ int ef_plan_set_sync_group(ef_plan *plan, int tiles);
  */
 int ef_plan_last_fallbacks(ef_plan *plan, unsigned int *parked_tiles, unsigned int *late_blocks);
 
+/*
+ * Which kernels ef_gated_forward and ef_gated_backward take in calls of the calling thread, in place of those that cost least; -1: those.
+ *   forward   0: for few tokens;  1, 2, 3: tiles of 256, 128 and 64 tokens
+ *   backward  0, 1, 2, 3: tiles of 256 x 256, 256 channels x 128 tokens, 128 x 128, 64 x 64
+ *   splits    parts along what the backward product sums over, as far as there are steps and room for them; 0: those that cost least
+ * EF_ERR_ARG for other values, which change nothing.
+ */
+int ef_gated_kernels(int forward, int backward, int splits);
+
 #ifdef __cplusplus
 }
 #endif

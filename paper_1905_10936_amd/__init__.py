@@ -43,7 +43,7 @@ ABI_SYMBOLS = (
 # ... and what include/ef_debug.h declares (tuning and diagnostics the tests use)
 DEBUG_SYMBOLS = (
     "ef_plan_tune", "ef_plan_fuse_limit", "ef_plan_set_persistent", "ef_plan_is_persistent", "ef_plan_set_sync_group",
-    "ef_plan_last_fallbacks", "ef_plan_small_calls", "ef_plan_server_pairs",
+    "ef_plan_last_fallbacks", "ef_plan_small_calls", "ef_plan_server_pairs", "ef_gated_kernels",
 )
 
 

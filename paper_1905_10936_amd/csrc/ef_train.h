@@ -30,6 +30,12 @@ struct TileShape {
     }
 };
 
+// What ef_gated_kernels has set.
+struct GatedChoice {
+    int forward = -1, backward = -1, splits = 0;
+};
+thread_local GatedChoice gated_choice;
+
 template <class T, int WC, int WT>
 void launch_gated(ef::GatedArgs a, hipStream_t s)
 {
@@ -67,6 +73,7 @@ void launch_gated(const ef::GatedArgs &a, hipStream_t s)
             best = i;
         }
     }
+    if (gated_choice.forward >= 0) best = gated_choice.forward - 1;
     if (best == 0)
         launch_gated<T, 4, 4>(a, s);
     else if (best == 1)
@@ -92,13 +99,14 @@ InputCut input_cut(int type, int64_t rows, int64_t n, int64_t steps)
     InputCut best{};
     double least = 0.0;
     for (const TileShape &c : SHAPES[type == EF_TYPE_BF16]) {
+        if (gated_choice.backward >= 0 && &c != &SHAPES[type == EF_TYPE_BF16][gated_choice.backward]) continue;
         const int64_t tiles = ceil_div(rows, 64 * c.wt) * ceil_div(n, 64 * c.wc);
         if (tiles > TILES_MAX) continue;
         for (int64_t splits = 1; splits <= 64 && splits <= steps; ++splits) {
             if (splits > 1 && splits * rows * n > PART_FLOATS) break;
             const double cost = c.cost(tiles * splits, ceil_div(steps, splits)) +
                                 (splits > 1 ? 4.0 + (double)(splits + 1) * (double)(rows * n) * 4.0 / 4.5e6 : 0.0);
-            if (!best.splits || cost < least) {
+            if (!best.splits || cost < least || splits <= gated_choice.splits) {
                 best = InputCut{c.wc, c.wt, (int)splits};
                 least = cost;
             }
@@ -242,6 +250,13 @@ int ef_gated_backward(ef_workspace *workspace, int64_t rows, int64_t width, int6
         EF_BY_TYPE(type, T, launch_input_grad<T>(a, s));
     }
     EF_HIP(hipGetLastError());
+    return EF_OK;
+}
+
+int ef_gated_kernels(int forward, int backward, int splits)
+{
+    if (forward < -1 || forward > 3 || backward < -1 || backward > 3 || splits < 0 || splits > 64) return EF_ERR_ARG;
+    gated_choice = GatedChoice{forward, backward, splits};
     return EF_OK;
 }
 

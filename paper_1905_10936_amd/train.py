@@ -24,7 +24,7 @@ def declare(L):
             ("ef_gated_forward", [i64, i64, i64, c_int, vp, i64, vp, i64, c_int, vp, i64, vp, i64, vp, vp]),
             ("ef_gated_backward", [vp, i64, i64, i64, c_int, vp, i64, vp, i64, vp, i64, c_int, vp, i64, vp, i64, vp]),
             ("ef_sample_tokens", [vp, i64, i64, c_int, vp, i64, vp, vp, vp, vp, vp, vp, vp, vp]),
-            ("ef_grad_clip", [vp, c_int, i64, vp, vp, vp, f32, vp, i64, vp, vp])):
+            ("ef_grad_clip", [vp, c_int, i64, vp, vp, vp, f32, vp, i64, vp, vp]), ("ef_gated_kernels", [c_int, c_int, c_int])):
         getattr(L, name).restype = c_int
         getattr(L, name).argtypes = args
 
