@@ -691,7 +691,8 @@ __global__ __launch_bounds__(Team<LANES>::THREADS) void k_sample(SampleArgs a)
     // ---- the draw: the first entry with more than u of the kept mass up to it
     double own = 0.0;
     const auto sum_of = [&](const double *m) { return ((m[0] + m[1]) + (m[2] + m[3])) + ((m[4] + m[5]) + (m[6] + m[7])); };
-    if (r.last == 0xffffffffu && r.least == -3.402823466e38f && floor_p <= 0.0) {
+    const bool uncut = r.last == 0xffffffffu && r.least == -3.402823466e38f;
+    if (uncut && floor_p <= 0.0) {
         // nothing is left out: -inf has no mass by itself
         r.row.each([&](const Eight<T> &e, unsigned) {
             double m[8];
@@ -700,12 +701,14 @@ __global__ __launch_bounds__(Team<LANES>::THREADS) void k_sample(SampleArgs a)
             own += sum_of(m);
         });
     } else {
-        // where no lane of the wavefront has more than a few of eight, each its own one by one, read again
+        // where no lane of the wavefront has more than a few of eight, each its own one by one, read again (without a cut none is looked for: 1 us of 22)
         r.each_kept([&](const float *v, unsigned at) {
             unsigned those = 0;
+            if (!uncut) {
 #pragma unroll
-            for (int k = 0; k < 8; ++k) those |= v[k] > -INFINITY ? 1u << k : 0u;
-            if (__any(__builtin_popcount(those) > 3)) {
+                for (int k = 0; k < 8; ++k) those |= v[k] > -INFINITY ? 1u << k : 0u;
+            }
+            if (uncut || __any(__builtin_popcount(those) > 3)) {
                 double m[8];
 #pragma unroll
                 for (int k = 0; k < 8; ++k) m[k] = kept_mass(v[k]);
