@@ -250,7 +250,7 @@ struct Sampler {
     }
 
     // f(value, place) for the entries whose bits those_of(values, place of the first) sets, of eights with something kept: a lane has few, so it goes through its own, read
-    // again, and not through all eight with branches (a pass for 2000 of 50257 kept 7 us that way).
+    // again, and not through all eight with branches (top-k 2000 of 50257: 42 us that way, 37 so).
     template <class M, class F>
     __device__ __forceinline__ void each_of(M those_of, F f) const
     {
