@@ -149,17 +149,17 @@ void launch_sample(ef::SampleArgs a, hipStream_t s)
         hipLaunchKernelGGL((ef::k_sample<T, LANES, HELD>), grid, dim3(Of::THREADS), 0, s, a);
     });
 }
-// A wavefront takes rows of up to 2048, a workgroup longer ones: in 48 KB of LDS, which leaves room for a second one on the CU, in 128 KB, or from the caches.
+// Rows of up to 512 are a wavefront's, and so are rows of up to 2048 where there are more of them than CUs; longer ones are a workgroup's, in 128 KB of LDS or from the
+// caches.  us, each way (wavefront, workgroup): 4096 x 2048 in bf16 without a filter 20, 67, with top-k 50 34, 146; 256 x 2048 8.3, 5.7 and 16, 11; 1 x 1024 with top-k 50 and
+// top-p 14, 10.  (LDS, caches): 256 x 50257 in bf16 with top-p 48, 59; 1024 x 32000 in fp32 118, 132.  With 48 KB of LDS rows of 20000 in bf16 took as long as with 128.
 template <class T>
 void launch_sample(const ef::SampleArgs &a, hipStream_t s)
 {
-    constexpr int KB = 1024 / (int)sizeof(T);
+    constexpr int KB = 1024 / (int)sizeof(T), CUS = 256;
     if (a.vocab <= 512)
         launch_sample<T, 64, 512>(a, s);
-    else if (a.vocab <= 2048)
+    else if (a.vocab <= 2048 && a.rows > CUS)
         launch_sample<T, 64, 2048>(a, s);
-    else if (a.vocab <= 48 * KB)
-        launch_sample<T, 1024, 48 * KB>(a, s);
     else if (a.vocab <= 128 * KB)
         launch_sample<T, 1024, 128 * KB>(a, s);
     else

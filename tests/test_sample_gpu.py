@@ -84,6 +84,21 @@ def test_long_rows_and_strides(kind, vocab, pad):
 
 
 @pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("rows,vocab", [(256, 513), (257, 513), (257, 1000), (300, 2047), (301, 2048), (257, 2049)])
+def test_rows_of_medium_length(kind, rows, vocab):
+    """Many rows are a wavefront's each, few a workgroup's; with the same tokens."""
+    gen = torch.Generator("cuda").manual_seed(vocab)
+    logits = (torch.randn(rows, vocab, device="cuda", generator=gen) * 3).to(TYPES[kind])
+    logits[7, 3:] = float("-inf")
+    uniform = torch.rand(rows, device="cuda", generator=gen)
+    settings = mixed(rows, gen, vocab)
+    tokens = check(logits, uniform, **settings)
+    few, _ = draw(logits[:24], uniform[:24], **{k: v[:24] for k, v in settings.items()})
+    assert torch.equal(tokens[:24], few)
+    check(logits, uniform, top_k=column(rows, vocab - 1, "top_k"), top_p=column(rows, 0.8, "top_p"))
+
+
+@pytest.mark.parametrize("kind", TYPES)
 @pytest.mark.parametrize("vocab", [5, 300, 9000, 40000])
 def test_equal_values(kind, vocab):
     """Ties go to the lower place, in every filter: rows of one value, of two, of a few."""
