@@ -265,16 +265,18 @@ struct Sampler {
         });
     }
 
-    // A bin's number for a value: linear, from 0 for `origin` on, the last for all that is far.  `unit`: a power of two that keeps differences in fp32's range.
+    // A bin's number for a value: linear, from 0 for `origin` on, the last for all that is far.  `unit`: a power of two that keeps differences in fp32's range, and with it
+    // `origin` finite: next to an origin of 2^20 or more values are a sixteenth or more apart, which at a unit of 1 is beyond any range that asks for 2^100.  So no value up to `origin` has a place
+    // below 0; a bin's number is an index in any case.
     struct Scale {
         float unit, origin, factor;
         __device__ __forceinline__ float at(float v) const { return __builtin_fmaf(v, -unit, origin) * factor; }
-        __device__ __forceinline__ int bin(float v) const { return (int)fminf(at(v), (float)(Of::BINS - 1)); }
+        __device__ __forceinline__ int bin(float v) const { return (int)__builtin_amdgcn_fmed3f(at(v), 0.0f, (float)(Of::BINS - 1)); }
     };
     static __device__ __forceinline__ Scale scale_of(float origin, double range)
     {
         Scale x;
-        x.unit = range > 1e30 || fabsf(origin) > 1e37f ? 0x1p-20f : range < 1e-30 ? 0x1p100f : 1.0f;
+        x.unit = range > 1e30 || fabsf(origin) > 1e37f ? 0x1p-20f : range < 1e-30 && fabsf(origin) < 0x1p20f ? 0x1p100f : 1.0f;
         x.origin = origin * x.unit;
         x.factor = (float)fmin(Of::BINS / (range * (double)x.unit), 1e30);
         return x;
