@@ -583,7 +583,8 @@ int ef_gated_backward(ef_workspace *workspace, int64_t rows, int64_t width, int6
  *     tokens[t] <- the least place at which the probability of what is kept, added up by place, passes uniform[t] of its sum
  *     logp[t]   <- logits[t][token] - log(sum_v exp(logits[t][v])): the log-probability under the policy itself, without temperature and filters, as
  *                  ef_token_logp gives it and ef_policy_loss takes it for logp_old
- * temperature 0, or top_p of 0 or less, takes the order's first entry.  Probabilities are in 64 bits and their sums do not depend on an order:
+ * temperature 0, or top_p of 0 or less, takes the order's first entry.  Probabilities are each right to 2^-32 of themselves, are held in 64 bits, and are rounded there so that
+ * their sums do not depend on an order (in all by less than 2^-31 of what is kept, with more than 2^20 entries by less than 2^-51 of it for each):
  * equal calls draw equal tokens.  -inf rules an entry out.  A row without a distribution gets token -1 and logp NaN: one that holds
  * a NaN or +inf or nothing but -inf, or whose uniform is not in [0, 1), temperature not finite or below 0, top_p or min_p NaN.  (A token of -1
  * masks its row in ef_token_logp and ef_policy_loss.)

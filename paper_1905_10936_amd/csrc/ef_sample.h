@@ -5,8 +5,9 @@
 // bits would have a wavefront's atomics meet in one), and the order within the one bin where the count runs out; top-p's the same way by probability.  A bin with
 // too many entries is binned again between its least and largest value; one of a single value is settled by counting places.
 //
-// Probabilities are 2^((v - top) log2(e) / T) in 64 bits, rounded to multiples of a power of two so large that sums of a whole row are exact (SampleRow::grid): they
-// come out the same in whatever order they are added, by LDS atomics too.  In fp32 one draw in 300 over 50000 entries would go by the order of the sums.
+// Probabilities are 2^((v - top) log2(e) / T) in 64 bits, rounded to multiples of a power of two so large that sums of a whole row are exact (Sampler::grid): they
+// come out the same in whatever order they are added, by LDS atomics too.  In fp32 one draw in 300 over 50000 entries would go by the order of the sums.  That power goes by the row's
+// own sum: by the number of its entries, 131071 of e^-24.5 beside one of 1 (3e-6 in all) would each be rounded to none.
 // Sums and draws look only at what is kept; a team reads its row once and keeps it in LDS.
 //
 // A row of any length is bound by its CU's instructions, a pass over 50257 entries by 110 cycles for each of its inner loop: in bf16 on all CUs (256 rows) 9 us greedy, 16 with
@@ -629,45 +630,45 @@ __global__ __launch_bounds__(Team<LANES>::THREADS) void k_sample(SampleArgs a)
     r.powers = powers;
     r.least = -3.402823466e38f;
     r.last = 0xffffffffu;
-    // The policy's own sum, in fp32's exponentials: a term's error is its own, and the sums are in 64 bits.
-    double whole = 0.0;
-    if (a.logp) {
-        r.row.each([&](const Eight<T> &e, unsigned) {
+    // The grid of the masses: their sum has to stay below 2^52 times it.  No more than as many as entries can stay, none above 1: of n, what is rounded away is below n^2 2^-52.  From
+    // COUNTED on that would show, and the row's own sum is the bound: what stays then has, of the row's n entries, at least its share, and is off by less than n 2^-51 of itself.
+    // At temperature 1 logp's sum is that one; else it is 8 exponentials more to a pass, without logp a pass (256 x 50257 in bf16 22.2 -> 25.0 us; by eight times the largest of every
+    // eight 24.4, and 26.2 with logp, which takes 25.0).
+    constexpr double COUNTED = 1024.0;
+    const bool greedy = heat == 0.0f || top_p <= 0.0f || top_k == 1;
+    double most = top_k > 0 ? fmin((double)top_k, (double)a.vocab) : (double)a.vocab;
+    const bool by_sum = !greedy && most > COUNTED;
+    r.factor = 1.4426950408889634074 / (double)heat;
+    // The policy's own sum and, at another temperature, the masses', in fp32's exponentials: a term's error is its own, and the sums are in 64 bits.
+    double whole = 0.0, heated = 0.0;
+    if (a.logp || by_sum) {
+        const float factor = (float)fmin(r.factor, 1e30), first = a.logp || heat == 1.0f ? 1.44269504f : factor;
+        const bool both = a.logp && by_sum && heat != 1.0f;
+        const auto sum_of = [&](const Eight<T> &e, float factor) {
             float v[8];
 #pragma unroll
-            for (int k = 0; k < 8; ++k) v[k] = __builtin_amdgcn_exp2f((e[k] - top) * 1.44269504f);
-            whole += (double)(((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7])));
+            for (int k = 0; k < 8; ++k) v[k] = __builtin_amdgcn_exp2f((e[k] - top) * factor);
+            return (double)(((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7])));
+        };
+        r.row.each([&](const Eight<T> &e, unsigned) {
+            whole += sum_of(e, first);
+            if (both) heated += sum_of(e, factor);
         });
         double all;
         Of::upto(whole, s.wave_sum, all);
         whole = all;
+        if (both) Of::upto(heated, s.wave_sum, all);
+        if (by_sum) most = fmin(most, 1.01 * all);
     }
 
     // ---- what is kept
-    const bool greedy = heat == 0.0f || top_p <= 0.0f;
-    if (greedy || top_k == 1) {
+    if (greedy) {
         r.first_alone();
         if (threadIdx.x % LANES == 0) {
             a.tokens[row] = (int64_t)r.last;
             if (a.logp) a.logp[row] = (float)-log(whole);
         }
         return;
-    }
-    r.factor = 1.4426950408889634074 / (double)heat;
-    // The grid of the masses: their sum has to stay below 2^52 times it.  No more than as many as entries can stay, none above 1: of n, what is rounded away is below n^2 2^-54.  Where
-    // that would show, the sum itself is the bound.
-    double most = top_k > 0 ? fmin((double)top_k, (double)a.vocab) : (double)a.vocab;
-    if (most > 131072.0) {
-        const float factor = (float)fmin(r.factor, 1e30);
-        double own = 0.0, all;
-        r.row.each([&](const Eight<T> &e, unsigned) {
-            float v[8];
-#pragma unroll
-            for (int k = 0; k < 8; ++k) v[k] = __builtin_amdgcn_exp2f((e[k] - top) * factor);
-            own += (double)(((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7])));
-        });
-        Of::upto(own, s.wave_sum, all);
-        most = fmin(most, 1.01 * all);
     }
     r.grid = __builtin_amdgcn_ldexp(1.5, __builtin_amdgcn_frexp_exp(most));
     if (top_k > 0 && top_k < a.vocab) {
