@@ -12,8 +12,9 @@
 
 namespace {
 
-constexpr int64_t ROWS_AT_ONCE = 1 << 22;       // tokens to a launch of a product: a grid holds less than 2^32 threads
-constexpr int64_t TILES_MAX = 1 << 22;
+constexpr int64_t TILES_MAX = 1 << 22;          // tiles to a launch of a product: a grid holds less than 2^32 threads
+// Tokens to a launch: no more than 2^22, and no more than the largest tiles (256 tokens by 128 channels) take.
+int64_t rows_at_once(int64_t channels) { return std::min(TILES_MAX / ceil_div(channels, 128) * 256, (int64_t)1 << 22); }
 
 // A tile of a product, 64 wc channels by 64 wt tokens, and what it was measured to take: a step (128 bytes of what is summed over) `alone` us with few workgroups
 // on the GPU and `loaded` us with as many as it holds (`most` on a CU; more slow the others down with the square of their share), a workgroup's beginning
@@ -169,9 +170,7 @@ void launch_sample(const ef::SampleArgs &a, hipStream_t s)
 int gated_sizes(int64_t rows, int64_t width, int64_t inner, int type, int gate)
 {
     if (rows < 0 || rows > ROWS_MAX || width < 1 || inner < 1 || !good_type(type) || (gate != EF_GATE_SILU && gate != EF_GATE_GELU)) return EF_ERR_ARG;
-    // the largest tiles of as many tokens as go into a launch: more would be beyond any memory
-    if (width > WIDTH_MAX || inner > WIDTH_MAX || ceil_div(std::min(rows, ROWS_AT_ONCE), 256) * ceil_div(std::max(width, inner), 128) > TILES_MAX) return EF_ERR_SIZE;
-    return EF_OK;
+    return width > WIDTH_MAX || inner > WIDTH_MAX ? EF_ERR_SIZE : EF_OK;
 }
 
 int good_matrices(std::initializer_list<const Matrix *> ms)
@@ -204,14 +203,15 @@ int ef_gated_forward(int64_t rows, int64_t width, int64_t inner, int type, const
     if (!apart(out, 3, in, 2, in_place)) return EF_ERR_ARG;
     if (!rows) return EF_OK;
     const ef::ActRef whole = act_ref(act, rows, inner);
-    for (int64_t first = 0; first < rows; first += ROWS_AT_ONCE) {
+    const int64_t most = rows_at_once(inner);
+    for (int64_t first = 0; first < rows; first += most) {
         const auto from = [&](auto *p, int64_t stride) { return p ? reinterpret_cast<decltype(p)>(reinterpret_cast<uintptr_t>(p) + (size_t)(first * stride) * size) : p; };
         ef::ActRef part = whole;
         if (act) {
             part.codes = whole.code_at(first, 0);
             part.scales = whole.scale_at(first, 0);
         }
-        const ef::GatedArgs a{std::min(rows - first, ROWS_AT_ONCE), width, inner, from(x, x_stride), x_stride, w, w_stride, gate, from(pre, pre_stride), pre_stride,
+        const ef::GatedArgs a{std::min(rows - first, most), width, inner, from(x, x_stride), x_stride, w, w_stride, gate, from(pre, pre_stride), pre_stride,
                               from(z, z_stride), z_stride, part, 0, 0};
         EF_BY_TYPE(type, T, launch_gated<T>(a, static_cast<hipStream_t>(stream)));
     }
@@ -243,9 +243,10 @@ int ef_gated_backward(ef_workspace *workspace, int64_t rows, int64_t width, int6
     });
     EF_HIP(hipGetLastError());
     if (!dx) return EF_OK;
-    for (int64_t first = 0; first < rows; first += ROWS_AT_ONCE) {
+    const int64_t most = rows_at_once(width);
+    for (int64_t first = 0; first < rows; first += most) {
         const auto from = [&](void *p, int64_t stride) { return static_cast<void *>(static_cast<char *>(p) + (size_t)(first * stride) * size); };
-        const ef::InputGradArgs a{std::min(rows - first, ROWS_AT_ONCE), width, 2 * inner, from(dpre, dpre_stride), dpre_stride, w, w_stride, from(dx, dx_stride), dx_stride, 0, 0, 1,
+        const ef::InputGradArgs a{std::min(rows - first, most), width, 2 * inner, from(dpre, dpre_stride), dpre_stride, w, w_stride, from(dx, dx_stride), dx_stride, 0, 0, 1,
                                   workspace->parts};
         EF_BY_TYPE(type, T, launch_input_grad<T>(a, s));
     }
