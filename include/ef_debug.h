@@ -111,6 +111,7 @@ int ef_plan_last_fallbacks(ef_plan *plan, unsigned int *parked_tiles, unsigned i
  *   forward   0: for few tokens;  1, 2, 3: tiles of 256, 128 and 64 tokens
  *   backward  0, 1, 2, 3: tiles of 256 x 256, 256 channels x 128 tokens, 128 x 128, 64 x 64
  *   splits    parts along what the backward product sums over, as far as there are steps and room for them; 0: those that cost least
+ * A kernel whose tiles of a call a grid does not hold is not taken for it.
  * EF_ERR_ARG for other values, which change nothing.
  */
 int ef_gated_kernels(int forward, int backward, int splits);

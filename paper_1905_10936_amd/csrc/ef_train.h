@@ -64,7 +64,7 @@ void launch_gated(const ef::GatedArgs &a, hipStream_t s)
     const double round = sizeof(T) == 2 ? 1.6 + 3.9 * (double)a.n / 1024.0 : 1.5 + 9.5 * (double)a.n / 1024.0;
     const int64_t few = ceil_div(a.rows, 32) * ceil_div(a.f, 16);
     double least = few <= TILES_MAX ? 1.5 + round * (double)ceil_div(few, 256) : 1e30;
-    int best = -1;
+    int best = -1, asked = gated_choice.forward == 0 && few > TILES_MAX ? -1 : gated_choice.forward;
     for (int i = 0; i < 3; ++i) {
         const TileShape &c = SHAPES[sizeof(T) == 2][i];
         const int64_t tiles = ceil_div(a.rows, 64 * c.wt) * ceil_div(a.f, 32 * c.wc);
@@ -73,8 +73,9 @@ void launch_gated(const ef::GatedArgs &a, hipStream_t s)
             least = cost;
             best = i;
         }
+        if (asked == i + 1 && tiles > TILES_MAX) asked = -1;
     }
-    if (gated_choice.forward >= 0) best = gated_choice.forward - 1;
+    if (asked >= 0) best = asked - 1;
     if (best == 0)
         launch_gated<T, 4, 4>(a, s);
     else if (best == 1)
@@ -97,11 +98,13 @@ InputCut input_cut(int type, int64_t rows, int64_t n, int64_t steps)
 {
     static constexpr TileShape SHAPES[2][4] = {{{4, 4, 1, 7.1, 7.3, 7.0}, {4, 2, 1, 3.7, 3.8, 5.0}, {2, 2, 2, 2.0, 3.8, 2.0}, {1, 1, 4, 0.57, 1.9, 1.0}},
                                                {{4, 4, 1, 1.1, 1.5, 7.0}, {4, 2, 1, 0.65, 0.95, 5.0}, {2, 2, 2, 0.43, 1.1, 2.0}, {1, 1, 4, 0.28, 0.84, 1.0}}};
+    const auto tiles_of = [&](const TileShape &c) { return ceil_div(rows, 64 * c.wt) * ceil_div(n, 64 * c.wc); };
+    const TileShape *const shapes = SHAPES[type == EF_TYPE_BF16], *const asked = gated_choice.backward >= 0 ? shapes + gated_choice.backward : nullptr;
     InputCut best{};
     double least = 0.0;
     for (const TileShape &c : SHAPES[type == EF_TYPE_BF16]) {
-        if (gated_choice.backward >= 0 && &c != &SHAPES[type == EF_TYPE_BF16][gated_choice.backward]) continue;
-        const int64_t tiles = ceil_div(rows, 64 * c.wt) * ceil_div(n, 64 * c.wc);
+        if (asked && &c != asked && tiles_of(*asked) <= TILES_MAX) continue;
+        const int64_t tiles = tiles_of(c);
         if (tiles > TILES_MAX) continue;
         for (int64_t splits = 1; splits <= 64 && splits <= steps; ++splits) {
             if (splits > 1 && splits * rows * n > PART_FLOATS) break;

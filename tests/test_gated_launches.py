@@ -92,3 +92,18 @@ def run(tmp_path_factory):
 def test_every_width_is_taken(run):
     """Widths up to 2^24 with any number of tokens: in launches of as many tokens as their grid takes."""
     run(SIZES)
+
+
+KERNELS = DRIVER + r"""
+for kernel in range(4):
+    assert L.ef_gated_kernels(kernel, kernel, 0) == 0
+    for rows, channels in ((1, 1), (100, 1 << 24), (8192, 1 << 24), (1 << 22, 32768), (1 << 23, 300)):
+        forward(rows, 1, channels, True, True)
+        backward(workspace, rows, channels, 1)
+print("launches ok")
+"""
+
+
+def test_kernels_that_are_asked_for(run):
+    """Where a grid does not hold their tiles another one is taken."""
+    run(KERNELS)
