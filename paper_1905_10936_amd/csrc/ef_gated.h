@@ -154,12 +154,14 @@ __global__ __launch_bounds__(PRODUCT_THREADS, WC * WT > 4 ? 1 : 2) void k_gated(
                     }
                 }
             }
+            Rows::meet();
             if (g.z) Rows::template flush<INSIDE>(mine, lane, static_cast<T *>(g.z) + t1 * g.z_stride + c1, g.z_stride, rows, left);
             if (g.pre) {
                 T *const to = static_cast<T *>(g.pre) + t1 * g.pre_stride + c1;
                 Rows::template flush<INSIDE>(mine + Rows::BYTES, lane, to, g.pre_stride, rows, left);
                 Rows::template flush<INSIDE>(mine + 2 * Rows::BYTES, lane, to + g.f, g.pre_stride, rows, left);
             }
+            Rows::meet();
         }
     };
     if (t0 + TILE_T <= g.rows && c0 + TILE_C <= g.f)
@@ -357,7 +359,9 @@ __global__ __launch_bounds__(PRODUCT_THREADS, WC * WT > 4 ? 1 : 2) void k_input_
                     for (int k = 0; k < 4; ++k) v[k] = acc[i][j][4 * r + k];
                     Rows::put(mine, lane, 32 * i + run_channel(lane, r), v);
                 }
+            Rows::meet();
             Rows::template flush<INSIDE>(mine, lane, to + t1 * stride + c1, stride, rows, left);
+            Rows::meet();
         }
     };
     const bool inside = t0 + TILE_T <= g.rows && c0 + TILE_C <= g.n;

@@ -283,6 +283,12 @@ __device__ __forceinline__ void product_steps(A &a, B &b, char *lds, int64_t fir
 template <class T, int CHANNELS>
 struct StagedRows {
     static constexpr int PITCH = CHANNELS * (int)sizeof(T) + 16, BYTES = 32 * PITCH, CHUNKS = CHANNELS / WORD<T>, EACH = 64 / CHUNKS;
+    // Between put() and flush(), and before the next put(): other lanes' words are read.  A wavefront's LDS operations are carried out in their order, so the compiler alone is to keep it.
+    static __device__ __forceinline__ void meet()
+    {
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+    }
     // four channels from c on of the lane's token
     static __device__ __forceinline__ void put(char *at, int lane, int c, const float *v)
     {
