@@ -542,7 +542,7 @@ int ef_policy_loss(ef_workspace *workspace, int64_t rows, int64_t vocab, int typ
  *     z  <- act(a) * u,            act(a) = a * sigmoid(F(a))
  *     pre <- a and u side by side,   act <- checkpoint of z
  * F(a) = a with EF_GATE_SILU, 2 sqrt(2 / pi) (a + 0.044715 a^3) with EF_GATE_GELU (the tanh form of GELU). z is made from a and u
- * before they are rounded; z and pre are rounded once to `type`, the checkpoint is of z before that.  The weights are of the activations'
+ * before they are rounded; z and pre are rounded once to `type`, the checkpoint is of z before that.  A sigmoid below 2^-126 may be taken as 0 (in bf16 it is).  The weights are of the activations'
  * type: a caller that keeps fp32 parameters casts them once a step.  Products of bf16 and of fp32 numbers enter exactly as the
  * type has them, and are summed in fp32.
  *
