@@ -10,8 +10,9 @@
 // own sum: by the number of its entries, 131071 of e^-24.5 beside one of 1 (3e-6 in all) would each be rounded to none.
 // Sums and draws look only at what is kept; a team reads its row once and keeps it in LDS.
 //
-// A row of any length is bound by its CU's instructions, a pass over 50257 entries by 110 cycles for each of its inner loop: in bf16 on all CUs (256 rows) 9 us greedy, 16 with
-// top-k 50, 22 with no filter, 40 with top-k 2000, 48 with top-p alone, where the bytes take 5; one row takes 2 to 6 us less.  64 rows of 128256 in fp32, top-p: 100.
+// A row of any length is bound by its CU's instructions, a pass over 50257 entries by 110 cycles for each of its inner loop: in bf16 on all CUs (256 rows) without logp 9 us greedy, 17
+// with top-k 50, 25 with no filter, 44 with top-k 2000, 51 with top-p alone, where the bytes take 5 (logp: 3 more for the first two, else nothing); one row takes 2 to 5 us less.  64 rows of 128256 in
+// fp32, top-p: 106.
 #pragma once
 #include "ef_rows.h"
 
@@ -254,7 +255,7 @@ struct Sampler {
     }
 
     // f(value, place) for the entries whose bits those_of(values, place of the first) sets, of eights with something kept: a lane has few, so it goes through its own, read
-    // again, and not through all eight with branches (top-k 2000 of 50257: 42 us that way, 37 so).
+    // again, and not through all eight with branches (top-k 2000 of 50257: 5 us more that way).
     template <class M, class F>
     __device__ __forceinline__ void each_of(M those_of, F f) const
     {
@@ -707,7 +708,7 @@ __global__ __launch_bounds__(Team<LANES>::THREADS) void k_sample(SampleArgs a)
             own += sum_of(m);
         });
     } else {
-        // where no lane of the wavefront has more than a few of eight, each its own one by one, read again (without a cut none is looked for: 1 us of 22)
+        // where no lane of the wavefront has more than a few of eight, each its own one by one, read again (without a cut none is looked for: 1 us of 25)
         r.each_kept([&](const float *v, unsigned at) {
             unsigned those = 0;
             if (!uncut) {

@@ -154,8 +154,8 @@ void launch_sample(ef::SampleArgs a, hipStream_t s)
     });
 }
 // Rows of up to 512 are a wavefront's, and so are rows of up to 2048 where there are more of them than CUs; longer ones are a workgroup's, in 128 KB of LDS or from the
-// caches.  us, each way (wavefront, workgroup): 4096 x 2048 in bf16 without a filter 20, 67, with top-k 50 34, 146; 256 x 2048 8.3, 5.7 and 16, 11; 1 x 1024 with top-k 50 and
-// top-p 14, 10.  (LDS, caches): 256 x 50257 in bf16 with top-p 48, 59; 1024 x 32000 in fp32 118, 132.  With 48 KB of LDS rows of 20000 in bf16 took as long as with 128.
+// caches.  us with logp, each way (wavefront, workgroup): 4096 x 2048 in bf16 without a filter 23, 80, with top-k 50 36, 160; 256 x 2048 9.0, 6.1 and 17, 12; 1 x 1024 with top-k 50 and
+// top-p 14, 11.  (LDS, caches): 256 x 50257 in bf16 with top-p 52, 65; 1024 x 32000 in fp32 125, 141.  Many rows of just over 2048 pay for it: 4096 x 2049 takes 87 without a filter and 164 with top-k 50.  With 48 KB of LDS rows of 20000 in bf16 took as long as with 128.
 template <class T>
 void launch_sample(const ef::SampleArgs &a, hipStream_t s)
 {
