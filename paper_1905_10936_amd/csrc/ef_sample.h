@@ -644,11 +644,13 @@ __global__ __launch_bounds__(Team<LANES>::THREADS) void k_sample(SampleArgs a)
     double whole = 0.0, heated = 0.0;
     if (a.logp || by_sum) {
         const float factor = (float)fmin(r.factor, 1e30), first = a.logp || heat == 1.0f ? 1.44269504f : factor;
+        // by halves: a difference beyond fp32 is none of no weight at the highest temperatures, and the bound is one
+        const float half = 0.5f * top;
         const bool both = a.logp && by_sum && heat != 1.0f;
         const auto sum_of = [&](const Eight<T> &e, float factor) {
             float v[8];
 #pragma unroll
-            for (int k = 0; k < 8; ++k) v[k] = __builtin_amdgcn_exp2f((e[k] - top) * factor);
+            for (int k = 0; k < 8; ++k) v[k] = __builtin_amdgcn_exp2f(__builtin_fmaf(e[k], 0.5f, -half) * (2.0f * factor));
             return (double)(((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7])));
         };
         r.row.each([&](const Eight<T> &e, unsigned) {

@@ -3,7 +3,8 @@ was never written shows."""
 import pytest
 import torch
 
-from tests.test_sample_gpu import TYPES, check, column
+from tests import train_oracle as oracle
+from tests.test_sample_gpu import TYPES, check, column, draw
 
 pytestmark = pytest.mark.gpu
 
@@ -31,3 +32,28 @@ def test_temperatures_next_to_0(kind, vocab):
             check(logits, uniform, temperature=column(rows, heat, "temperature"), top_p=column(rows, 0.5, "top_p"))
         check(logits, uniform, temperature=column(rows, heat, "temperature"), top_k=column(rows, vocab // 2, "top_k"), top_p=column(rows, 0.3, "top_p"))
     check(logits, uniform, temperature=column(rows, 3e36, "temperature"), top_p=column(rows, 0.5, "top_p"))
+
+
+@pytest.mark.parametrize("vocab", [1500, 20000, 140000])
+@pytest.mark.parametrize("kind", TYPES)
+def test_differences_beyond_fp32(kind, vocab):
+    """Logits from one end of the type to the other at a temperature that leaves each its weight: sums are exact, so that the same rows in another place, with the
+    log-probabilities or without, have the same tokens, the oracle's.  (The log-probabilities themselves are beyond fp32.)"""
+    gen = torch.Generator("cuda").manual_seed(vocab)
+    rows, most = 16, torch.finfo(TYPES[kind]).max
+    logits = ((torch.rand(rows, vocab, device="cuda", generator=gen, dtype=torch.float64) * 2 - 1) * most).to(TYPES[kind])
+    logits[::2] = torch.where(torch.rand(rows // 2, vocab, device="cuda", generator=gen) < 0.5, -most, -0.9 * most).to(TYPES[kind])
+    logits[:, 3] = most
+    uniform = torch.rand(rows, device="cuda", generator=gen)
+    for heat in (3e38, 1e38):
+        for p in (1.0, 0.7, 0.2):
+            settings = {"temperature": column(rows, heat, "temperature"), "top_p": column(rows, p, "top_p")}
+            tokens, logp = draw(logits, uniform, **settings)
+            v, u = logits.double().cpu().numpy(), uniform.double().cpu().numpy()
+            for i in range(rows):
+                assert int(tokens[i]) in oracle.sample(v[i], u[i], heat=float(settings["temperature"][i]), p=float(settings["top_p"][i]))[0], (heat, p, i)
+            assert not torch.isnan(logp).any()
+            for _ in range(3):
+                turned = torch.randperm(rows, device="cuda", generator=gen)
+                again, _ = draw(logits[turned], uniform[turned], logp=False, **settings)
+                assert torch.equal(again, tokens[turned])
