@@ -644,7 +644,7 @@ __global__ __launch_bounds__(Team<LANES>::THREADS) void k_sample(SampleArgs a)
     double whole = 0.0, heated = 0.0;
     if (a.logp || by_sum) {
         const float factor = (float)fmin(r.factor, 1e30), first = a.logp || heat == 1.0f ? 1.44269504f : factor;
-        // by halves: a difference beyond fp32 is none of no weight at the highest temperatures, and the bound is one
+        // by halves, which keeps differences within fp32: at the highest temperatures an entry at the type's other end has weight
         const float half = 0.5f * top;
         const bool both = a.logp && by_sum && heat != 1.0f;
         const auto sum_of = [&](const Eight<T> &e, float factor) {
